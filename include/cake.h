@@ -526,6 +526,106 @@ int32_t cake_op_decode_attention(cake_ctx* ctx, const float* q, float* out, int3
 int32_t cake_op_decode_attention_static(cake_ctx* ctx, const float* q, float* out, int32_t layer,
                                         int32_t n_keys, const cake_kv* kv);
 
+/* ---- decoding a batch from an 8-bit cache ------------------------------ */
+
+/* What follows the first token: a batch of sequences whose KV is kept in 8 bits, appended to and read token by token (or
+ * prompt piece by prompt piece), and the choice of each next token.  All calls are asynchronous on the compute stream, allocate nothing
+ * and may be captured into a graph; like all launches of a context they use its workspace, so graphs captured from one
+ * context are replayed one after another.
+ *
+ * Pool: layer page (layer, page) at pool + (layer * n_physical_pages + page) * cake_q8_page_bytes, 16-byte aligned:
+ *     K codes  int8    [kv_head][token_in_page][head_dim]
+ *     K scales float32 [kv_head][token_in_page / scale_tokens]
+ *     V codes, V scales likewise (V not transposed)
+ * value = code * scale, scale = largest magnitude of the block of scale_tokens tokens / 127.  With scale_tokens = 1 the bytes are
+ * those of the CAKE_STORE_INT8 image of that layer.
+ *
+ * The arrays of the batch are read on the device when the work runs, so a captured step goes on with what they hold then.
+ * Sequence s has seq_len[s] tokens, the new ones included; rows row_begin[s] .. row_begin[s + 1] - 1 of the batch are its LAST
+ * tokens.  Rows before row_begin[0] and from row_begin[n_seqs] on belong to no sequence: nothing of theirs is written.
+ * What the arrays hold is not trusted: a page number outside the pool, or a length beyond the block table, is never followed
+ * (append writes nothing there, rows that would see such keys come out as NaN); rows of a sequence in excess of its tokens
+ * stand for no token (append leaves theirs as they were, attention gives zeros).  Sequences may share pages that they only read. */
+typedef struct {
+    void* pool;                 /* device, 16-byte aligned */
+    const int32_t* block_table; /* device, [n_seqs][pages_per_seq]; entries past a sequence's last page are not read */
+    const int32_t* seq_len;     /* device, [n_seqs] */
+    const int32_t* row_begin;   /* device, [n_seqs + 1], not decreasing */
+    int32_t n_seqs;
+    int32_t pages_per_seq;
+    int32_t page_tokens;        /* a multiple of 64 */
+    int32_t scale_tokens;       /* tokens that share a scale: 1, 2, 4, .. 64; n_kv_heads * page_tokens / scale_tokens a multiple of 4 */
+    int32_t n_physical_pages;   /* pages per layer in the pool */
+    int32_t n_rows;             /* rows of the batch's activations */
+    int32_t max_rows;           /* most rows of one sequence and ... */
+    int32_t max_len;            /* ... most tokens of one: they choose kernels and launch sizes, results do not depend on them (0: unknown) */
+} cake_q8_batch;
+
+/* Bytes of one layer page, 0 if the sizes are not supported.  Pure. */
+uint64_t cake_q8_page_bytes(const cake_model_desc* model, int32_t page_tokens, int32_t scale_tokens);
+
+/* Rotary positions: of each head the first rotary_dim elements turn, in pairs (2i, 2i+1) or (i, i + rotary_dim/2), by position *
+ * freq[i]; cosine and sine are multiplied by magnitude. */
+typedef enum { CAKE_ROPE_PAIRS = 0, CAKE_ROPE_HALVES = 1 } cake_rope_layout;
+/* Frequencies f_i = theta^(-2i / rotary_dim), scaled for contexts longer than the model was trained on:
+ * CAKE_ROPE_PLAIN   f_i
+ * CAKE_ROPE_LINEAR  f_i / factor
+ * CAKE_ROPE_BANDS   by how often pair i turns within original_tokens, n_i = original_tokens f_i / 2 pi: f_i from `high` turns on,
+ *                   f_i / factor up to `low`, between them mixed in proportion to n_i
+ * CAKE_ROPE_RAMP    by the pair's number: f_i below the (real) number at which a pair turns `high` times within original_tokens,
+ *                   f_i / factor above that of `low` times, between (both rounded outwards to whole numbers inside
+ *                   [0, rotary_dim - 1]) in proportion; magnitude 0.1 ln(factor) + 1 */
+typedef enum { CAKE_ROPE_PLAIN = 0, CAKE_ROPE_LINEAR = 1, CAKE_ROPE_BANDS = 2, CAKE_ROPE_RAMP = 3 } cake_rope_scaling;
+typedef struct {
+    double theta;
+    double factor;              /* >= 1; PLAIN: not read */
+    double low, high;           /* BANDS, RAMP: turns, 0 < low < high */
+    int32_t rotary_dim;         /* even, 2 .. 128 */
+    int32_t layout;             /* cake_rope_layout */
+    int32_t scaling;            /* cake_rope_scaling */
+    int32_t original_tokens;    /* BANDS, RAMP */
+} cake_rope_desc;
+typedef struct {
+    double freq[64];
+    double magnitude;
+    int32_t rotary_dim;
+    int32_t layout;
+} cake_rope;
+/* Fills `out` (host).  Pure; no context, no GPU.  Errors: CAKE_E_INVAL. */
+int32_t cake_rope_init(cake_rope* out, const cake_rope_desc* desc);
+
+/* Appends the batch's new tokens to layer `layer`: q[n_q][n_rows][head_dim] (device, model dtype) = the rotated queries of
+ * qkv[n_rows][(n_q + 2 n_kv) head_dim] (device, float32), and the rotated keys and the values go into the pages as codes.  Row i of
+ * a sequence's rows is at position seq_len - rows + i.  Rotated in 64 bits and rounded to float32 once; scale and code are
+ * float32 quotients, codes rounded half to even.  A block that already holds earlier tokens keeps the larger of its scale and the
+ * new tokens'; where that is larger the earlier codes become rint(code * old / new).  A block with an infinity or a NaN gets a
+ * NaN scale.  values: device, [n_rows][2 n_kv][head_dim] in the model dtype, what the pages now stand for (K heads, then V heads;
+ * NaN where no page could be written), or NULL.  No two sequences may append to one page.  Pointers 16-byte aligned.
+ * Errors: CAKE_E_INVAL, CAKE_E_HIP. */
+int32_t cake_op_append_q8(cake_ctx* ctx, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope,
+                          const cake_q8_batch* batch);
+/* out[n_rows][n_q * head_dim] = attention of q[n_q][n_rows][head_dim] (both device, model dtype) over layer `layer`: the row at
+ * position p sees keys j <= p, with window > 0 only those with p - j < window or j < sinks.  A row that sees no key is zeros.  Scores,
+ * softmax and sums in float32; bf16 models round the weights to 16 bits or to 11 (of the largest) on the way into the second product.
+ * Pointers 16-byte aligned.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
+int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
+                             const cake_q8_batch* batch);
+
+/* The next token of each row of logits (device, float32, rows row_stride elements apart), all arrays device, [rows]:
+ *  - temperature T (NULL: 1); T <= 0 or NaN: the likeliest token, lowest id among equals, log-probability 0;
+ *  - top_k: the k likeliest stay (NULL, <= 0: all), equal logits ranked by id;
+ *  - top_p: of those, the fewest likeliest ones whose probabilities (of softmax(logits / T) over the first k) reach top_p
+ *    (NULL, >= 1 or NaN: all; <= 0: the likeliest);
+ *  - min_p: of those, the ones with at least min_p (at most 1) times the likeliest one's probability (NULL, <= 0 or NaN: all);
+ *  - u, a random number in [0, 1) (NaN counts as 0): the token is the first of those in the order of their ids whose running
+ *    probability exceeds u.
+ * A logit of -infinity or NaN is never chosen; with +infinity only those are.  A row with nothing to choose gives token -1 and
+ * log-probability -infinity.  tokens: int32; logprobs: float32, log of the token's probability among those that stayed, or NULL.
+ * Probabilities below 2^-45 of the likeliest one's count as 0.  The result does not depend on the batch that a row is in.
+ * vocab <= 2^19, row_stride >= vocab.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
+int32_t cake_op_sample(cake_ctx* ctx, const float* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
+                       const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tokens, float* logprobs);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,7 @@ EXPORTS = [
     "cake_op_gemm", "cake_op_gemm_residual", "cake_op_gemm_swiglu", "cake_op_gemm_plan", "cake_op_mfma_rate", "cake_device_info", "cake_op_rope_kv_write",
     "cake_op_attention", "cake_profile_enable", "cake_profile_read", "cake_adaptive_serve", "cake_first_token",
     "cake_op_decode_attention", "cake_op_decode_attention_static", "cake_set_traces", "cake_store_image_bytes", "cake_write_store", "cake_prefix_keys", "cake_prefix_lookup",
+    "cake_q8_page_bytes", "cake_rope_init", "cake_op_append_q8", "cake_op_attention_q8", "cake_op_sample",
 ]
 STORE_RAW, STORE_INT8, STORE_INT4 = 0, 1, 2
 STORE_PINNED, STORE_FILE = 0, 1
@@ -121,6 +122,26 @@ class Tuning(C.Structure):
                 ("kernel_path", C.c_int32), ("gemm_config", C.c_int32), ("attn_variant", C.c_int32), ("gemm_ksplit", C.c_int32)]
 
 
+class Q8Batch(C.Structure):
+    """cake_q8_batch; Engine.q8_batch makes one and keeps the tensors it points to."""
+    _fields_ = [(n, C.c_void_p) for n in ("pool", "block_table", "seq_len", "row_begin")] + \
+               [(n, C.c_int32) for n in ("n_seqs", "pages_per_seq", "page_tokens", "scale_tokens", "n_physical_pages", "n_rows", "max_rows",
+                                         "max_len")]
+
+
+ROPE_LAYOUTS = {"pairs": 0, "halves": 1}
+ROPE_SCALINGS = {"linear": 1, "bands": 2, "ramp": 3}
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("theta", "factor", "low", "high")] + \
+               [(n, C.c_int32) for n in ("rotary_dim", "layout", "scaling", "original_tokens")]
+
+
+class Rope(C.Structure):
+    _fields_ = [("freq", C.c_double * 64), ("magnitude", C.c_double), ("rotary_dim", C.c_int32), ("layout", C.c_int32)]
+
+
 def load_library():
     """Loads libcake.so and declares the prototypes.  Raises if it is not built."""
     global _lib
@@ -170,6 +191,11 @@ def load_library():
         "cake_device_info": (i32, [vp, P(i32), P(i32), P(C.c_uint64)]),
         "cake_op_rope_kv_write": (i32, [vp, vp, vp, i32, i32, i32, P(Kv)]),
         "cake_op_attention": (i32, [vp, vp, vp, i32, i32, i32, P(Kv)]),
+        "cake_q8_page_bytes": (u64, [P(ModelDesc), i32, i32]),
+        "cake_rope_init": (i32, [P(Rope), P(RopeDesc)]),
+        "cake_op_append_q8": (i32, [vp, vp, vp, vp, i32, P(Rope), P(Q8Batch)]),
+        "cake_op_attention_q8": (i32, [vp, vp, vp, i32, i32, i32, P(Q8Batch)]),
+        "cake_op_sample": (i32, [vp, vp, C.c_int64, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -256,6 +282,33 @@ def page_image_bytes(shape, page_tokens) -> int:
     return int(load_library().cake_page_image_bytes(C.byref(model_desc(shape)), page_tokens))
 
 
+def q8_page_bytes(shape, page_tokens, scale_tokens=1) -> int:
+    """Bytes of one layer page of an 8-bit cache (cake_q8_page_bytes)."""
+    n = int(load_library().cake_q8_page_bytes(C.byref(model_desc(shape)), page_tokens, scale_tokens))
+    if n == 0:
+        raise CakeError(E_INVAL, "cake_q8_page_bytes: pages of %d tokens with a scale for %d" % (page_tokens, scale_tokens))
+    return n
+
+
+def rope(theta, rotary_dim, layout="pairs", scaling=None) -> Rope:
+    """Rotary positions (cake_rope_init).  scaling: None, ("linear", factor), ("bands", factor, low, high, original_tokens) or
+    ("ramp", factor, original_tokens, high, low); see cake_rope_scaling."""
+    d, kind = RopeDesc(theta=theta, rotary_dim=rotary_dim, layout=ROPE_LAYOUTS[layout]), scaling[0] if scaling else None
+    if kind:
+        d.scaling, d.factor = ROPE_SCALINGS[kind], scaling[1]
+        if kind == "linear":
+            (_, _) = scaling
+        elif kind == "bands":
+            d.low, d.high, d.original_tokens = scaling[2:]
+        else:
+            d.original_tokens, d.high, d.low = scaling[2:]
+    out = Rope()
+    rc = load_library().cake_rope_init(C.byref(out), C.byref(d))
+    if rc != OK:
+        raise CakeError(rc, "cake_rope_init")
+    return out
+
+
 # --------------------------------------------------------------------------- device side
 @dataclass
 class PrefillResult:
@@ -286,10 +339,12 @@ class Engine:
     """Owns the device tensors (weights in ABI layout, KV pool, block tables), the pinned
     store and the two streams, and forwards to the C ABI.  The op_* calls wait for what torch's current
     stream was given before them (their operands come from there); the others do not: synchronise
-    after torch has written to the pool."""
+    after torch has written to the pool.  op_append_q8, op_attention_q8 and op_sample return before their work is done: it runs
+    in order with torch's current stream, without a wait where that is the compute stream.
+    compute_stream: a torch stream of the default priority to use as the compute stream (None: one of the engine's own)."""
 
     def __init__(self, shape, weights=None, *, max_tokens, max_chunk, page_tokens=256, block_table=None,
-                 n_physical_pages=None, device="cuda:0", seed=0, with_head=False):
+                 n_physical_pages=None, device="cuda:0", seed=0, with_head=False, compute_stream=None):
         import torch
         self.torch = torch
         self.lib = load_library()
@@ -301,7 +356,7 @@ class Engine:
         self.tdtype = torch.float32 if shape.dtype == "f32" else torch.bfloat16
         self.page_tokens = page_tokens
         self.max_tokens, self.max_chunk = max_tokens, max_chunk
-        self._take_streams()
+        self._take_streams(compute_stream)
         self._tensors = []
         self.with_head = with_head or (weights is not None and "lm_head" in weights)
         self._build_weights(weights, seed)
@@ -354,14 +409,16 @@ class Engine:
             spare.append(stream)
         return spare.pop()
 
-    def _take_streams(self):
+    def _take_streams(self, compute_stream):
         """A compute stream beside those of the two engines before, and a copy stream beside it.  (Where only the copy
         stream was looked at, a third engine's compute stream met the first's on its queue, and small products of three
         engines in turn took 16.5 us each instead of 12.9.)"""
         with self._streams_lock:
             recent = self._recent.setdefault(self.dev, [])
-            self.compute_stream = self._take_stream(recent)
+            self.compute_stream = compute_stream or self._take_stream(recent)
             self.copy_stream = self._take_stream([self.compute_stream])
+            if compute_stream is not None:
+                return
             recent.append(self.compute_stream)
             del recent[:-2]
 
@@ -748,6 +805,85 @@ class Engine:
                                                C.byref(self.kv)), "cake_op_attention")
         self.sync()
         return out
+
+    # -- a ragged batch over an 8-bit cache ---------------------------------------------
+    def _in_order(self, call, what):
+        """A call whose work is to run between what torch's current stream has and what it gets next."""
+        current = self.torch.cuda.current_stream(self.dev)
+        same = current.cuda_stream == self.compute_stream.cuda_stream
+        if not same:
+            self.compute_stream.wait_stream(current)
+        rc = call()
+        if not same:
+            current.wait_stream(self.compute_stream)
+        self._check(rc, what)
+
+    def _operand(self, t, name, dtype, shape=None):
+        """Address of a contiguous tensor on the engine's device, or a refusal."""
+        if t.dtype != dtype or t.device != self.dev or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+            raise CakeError(E_INVAL, "%s: a contiguous %s tensor%s on %s is needed, got %s %s on %s" % (
+                name, dtype, "" if shape is None else " of %s" % (tuple(shape),), self.dev, t.dtype, tuple(t.shape), t.device))
+        return t.data_ptr()
+
+    def new_q8_pool(self, n_pages, page_tokens, scale_tokens=1):
+        """A pool of 8-bit pages, zeros: uint8 [n_layers][n_pages][page bytes]."""
+        return self.torch.zeros((self.shape.n_layers, n_pages, q8_page_bytes(self.shape, page_tokens, scale_tokens)),
+                                dtype=self.torch.uint8, device=self.dev)
+
+    def q8_batch(self, pool, block_table, seq_len, row_begin, *, n_rows, page_tokens, scale_tokens=1, max_rows=0, max_len=0) -> Q8Batch:
+        """The description of a batch for op_append_q8 and op_attention_q8 (cake_q8_batch).  pool: uint8 [n_layers *] pages x page
+        bytes; block_table: int32 [n_seqs][pages_per_seq]; seq_len: int32 [n_seqs]; row_begin: int32 [n_seqs + 1].  It may be kept
+        and used while the tensors stay; what they hold is read when the work runs."""
+        torch = self.torch
+        page = q8_page_bytes(self.shape, page_tokens, scale_tokens)
+        if pool.numel() == 0 or pool.numel() % (page * self.shape.n_layers):
+            raise CakeError(E_INVAL, "q8_batch: a pool of %d bytes for %d layers of pages of %d" % (pool.numel(), self.shape.n_layers, page))
+        if block_table.dim() != 2:
+            raise CakeError(E_INVAL, "q8_batch: block_table must have a row per sequence")
+        n = block_table.shape[0]
+        b = Q8Batch(self._operand(pool, "pool", torch.uint8), self._operand(block_table, "block_table", torch.int32),
+                    self._operand(seq_len, "seq_len", torch.int32, (n,)), self._operand(row_begin, "row_begin", torch.int32, (n + 1,)),
+                    n, block_table.shape[1], page_tokens, scale_tokens, pool.numel() // (page * self.shape.n_layers), n_rows, max_rows, max_len)
+        b.tensors = (pool, block_table, seq_len, row_begin)
+        return b
+
+    def op_append_q8(self, qkv, layer, batch, rope, q=None, want_values=False):
+        """qkv float32 [n_rows][(n_q + 2 n_kv) hd] -> q [n_q][n_rows][hd], rotated; keys and values into the pages.  want_values:
+        (q, values [n_rows][2 n_kv][hd] as the pages now hold them)."""
+        s, n = self.shape, batch.n_rows
+        if q is None:
+            q = self.torch.empty((s.n_q, n, s.head_dim), dtype=self.tdtype, device=self.dev)
+        values = self.torch.empty((n, 2 * s.n_kv, s.head_dim), dtype=self.tdtype, device=self.dev) if want_values else None
+        args = (self._operand(qkv, "qkv", self.torch.float32, (n, (s.n_q + 2 * s.n_kv) * s.head_dim)),
+                self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)), values.data_ptr() if want_values else None)
+        self._in_order(lambda: self.lib.cake_op_append_q8(self.ctx, *args, layer, C.byref(rope), C.byref(batch)), "cake_op_append_q8")
+        return (q, values) if want_values else q
+
+    def op_attention_q8(self, q, layer, batch, window=0, sinks=0, out=None):
+        """q [n_q][n_rows][hd] -> [n_rows][n_q * hd] (cake_op_attention_q8)."""
+        s, n = self.shape, batch.n_rows
+        if out is None:
+            out = self.torch.empty((n, s.n_q * s.head_dim), dtype=self.tdtype, device=self.dev)
+        args = (self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)), self._operand(out, "out", self.tdtype, (n, s.n_q * s.head_dim)))
+        self._in_order(lambda: self.lib.cake_op_attention_q8(self.ctx, *args, layer, window, sinks, C.byref(batch)), "cake_op_attention_q8")
+        return out
+
+    def op_sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+        """The next token of each row of logits (float32 [rows][vocab], rows any distance apart) and its log-probability; u and the
+        settings are tensors of a value per row (cake_op_sample)."""
+        torch = self.torch
+        if logits.dim() != 2 or logits.dtype != torch.float32 or logits.device != self.dev or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise CakeError(E_INVAL, "op_sample: logits must be float32 [rows][vocab] on %s with neighbouring elements side by side" % self.dev)
+        rows, vocab = logits.shape
+        tokens = torch.empty(rows, dtype=torch.int32, device=self.dev)
+        logprobs = torch.empty(rows, dtype=torch.float32, device=self.dev)
+        a = [None if t is None else self._operand(t, n, d, (rows,)) for t, n, d in (
+            (temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
+            (min_p, "min_p", torch.float32), (u, "u", torch.float32))]
+        stride = logits.stride(0) if rows > 1 else max(logits.stride(0), vocab)
+        self._in_order(lambda: self.lib.cake_op_sample(self.ctx, logits.data_ptr(), stride, rows, vocab, *a, tokens.data_ptr(),
+                                                       logprobs.data_ptr()), "cake_op_sample")
+        return tokens, logprobs
 
     def close(self):
         if getattr(self, "ctx", None) and self.ctx.value:

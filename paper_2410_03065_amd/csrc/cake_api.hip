@@ -1543,4 +1543,70 @@ int32_t cake_op_decode_attention_static(cake_ctx* c, const float* q, float* out,
     return CAKE_OK;
 }
 
+// ---- a ragged batch over an 8-bit cache ---------------------------------------------------
+static bool off16(const void* p) { return (uintptr_t(p) & 15) != 0; }
+
+// Checks what the host can see of a batch (its arrays are read on the device) and lays out the view of one layer.
+static int check_q8(cake_ctx* c, const char* what, const cake_q8_batch* b, int layer, Q8View* v, int* max_rows, int* max_len) {
+    if (layer < 0 || layer >= c->m.n_layers) return fail(c, CAKE_E_INVAL, "%s: layer %d of %d", what, layer, c->m.n_layers);
+    if (!b || !b->pool || (b->n_seqs > 0 && (!b->block_table || !b->seq_len || !b->row_begin))) return fail(c, CAKE_E_INVAL, "%s: batch: null pointer", what);
+    const uint64_t page = cake_q8_page_bytes(&c->m, b->page_tokens, b->scale_tokens);
+    if (!page) return fail(c, CAKE_E_INVAL, "%s: batch: pages of %d tokens with a scale for %d are not supported", what, b->page_tokens, b->scale_tokens);
+    if (off16(b->pool)) return fail(c, CAKE_E_INVAL, "%s: batch: the pool is not 16-byte aligned", what);
+    if (b->n_seqs < 0 || int64_t(b->n_seqs) * c->m.n_kv_heads > (1 << 26) || b->n_rows < 0 || b->n_rows > (1 << 28) || b->pages_per_seq <= 0 || b->n_physical_pages <= 0 ||
+        int64_t(b->pages_per_seq) * b->page_tokens > Q8_MOST_TOKENS)
+        return fail(c, CAKE_E_INVAL, "%s: batch: %d sequences of %d pages, %d rows, %d pages in the pool", what, b->n_seqs, b->pages_per_seq, b->n_rows, b->n_physical_pages);
+    if (b->max_rows < 0 || b->max_len < 0) return fail(c, CAKE_E_INVAL, "%s: batch: negative max_rows or max_len", what);
+    *v = Q8View{};
+    v->page_bytes = page; v->half_bytes = page / 2;
+    v->scales_off = size_t(c->m.n_kv_heads) * b->page_tokens * c->m.head_dim;
+    v->base = (unsigned char*)b->pool + size_t(layer) * b->n_physical_pages * page;
+    v->table = b->block_table; v->seq_len = b->seq_len; v->row_begin = b->row_begin;
+    v->n_seqs = b->n_seqs; v->pages_per_seq = b->pages_per_seq; v->page_tokens = b->page_tokens; v->n_phys = b->n_physical_pages;
+    v->n_kv = c->m.n_kv_heads; v->head_dim = c->m.head_dim; v->n_rows = b->n_rows;
+    while ((1 << v->scale_shift) < b->scale_tokens) ++v->scale_shift;
+    *max_rows = b->max_rows ? std::min(b->max_rows, b->n_rows) : b->n_rows;
+    *max_len = b->pages_per_seq * b->page_tokens;
+    if (b->max_len) *max_len = std::min(b->max_len, *max_len);
+    return CAKE_OK;
+}
+
+int32_t cake_op_append_q8(cake_ctx* c, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope, const cake_q8_batch* batch) {
+    if (!c) return CAKE_E_INVAL;
+    Q8View v;
+    int max_rows, max_len;
+    const int rc = check_q8(c, "op_append_q8", batch, layer, &v, &max_rows, &max_len);
+    if (rc != CAKE_OK) return rc;
+    if (!rope || rope->rotary_dim < 2 || rope->rotary_dim > c->m.head_dim || rope->rotary_dim % 2 || (rope->layout != CAKE_ROPE_PAIRS && rope->layout != CAKE_ROPE_HALVES))
+        return fail(c, CAKE_E_INVAL, "op_append_q8: rotary description: null, or not for heads of %d", c->m.head_dim);
+    if (v.n_rows == 0 || v.n_seqs == 0) return CAKE_OK;
+    if (!qkv || !q || off16(qkv) || off16(q) || off16(values)) return fail(c, CAKE_E_INVAL, "op_append_q8: qkv, q or values null or not 16-byte aligned");
+    HIP_TRY(c, launch_append_q8(c->m.dtype, qkv, q, values, v, *rope, c->m.n_q_heads, max_rows, c->cs));
+    return CAKE_OK;
+}
+
+int32_t cake_op_attention_q8(cake_ctx* c, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks, const cake_q8_batch* batch) {
+    if (!c) return CAKE_E_INVAL;
+    Q8View v;
+    int max_rows, max_len;
+    const int rc = check_q8(c, "op_attention_q8", batch, layer, &v, &max_rows, &max_len);
+    if (rc != CAKE_OK) return rc;
+    if (window < 0 || sinks < 0) return fail(c, CAKE_E_INVAL, "op_attention_q8: window %d, sinks %d", window, sinks);
+    if (v.n_rows == 0 || v.n_seqs == 0) return CAKE_OK;
+    if (!q || !out || off16(q) || off16(out)) return fail(c, CAKE_E_INVAL, "op_attention_q8: q or out null or not 16-byte aligned");
+    HIP_TRY(c, launch_attention_q8(c->m.dtype, q, out, v, c->m.n_q_heads, max_rows, max_len, window, sinks, AttnWs{c->split.part, c->split.part_bytes, 0}, c->cs));
+    return CAKE_OK;
+}
+
+int32_t cake_op_sample(cake_ctx* c, const float* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature, const int32_t* top_k,
+                       const float* top_p, const float* min_p, const float* u, int32_t* tokens, float* logprobs) {
+    if (!c) return CAKE_E_INVAL;
+    if (rows < 0 || rows > (1 << 20) || vocab <= 0 || vocab > SAMPLE_MOST_VOCAB || row_stride < vocab)
+        return fail(c, CAKE_E_INVAL, "op_sample: %d rows of %d logits, %lld apart", rows, vocab, (long long)row_stride);
+    if (rows == 0) return CAKE_OK;
+    if (!logits || !u || !tokens) return fail(c, CAKE_E_INVAL, "op_sample: null pointer");
+    HIP_TRY(c, launch_sample({logits, row_stride, rows, vocab, temperature, top_k, top_p, min_p, u, tokens, logprobs}, c->split.part, c->split.part_bytes, c->cs));
+    return CAKE_OK;
+}
+
 }  // extern "C"

@@ -1,4 +1,6 @@
 // Host-only entry points: the meet-point planner, the virtual-time race and size helpers.
+#include <algorithm>
+#include <cmath>
 #include <vector>
 
 #include "race_core.hpp"
@@ -101,6 +103,45 @@ uint64_t cake_store_image_bytes(const cake_model_desc* model, int32_t page_token
 uint64_t cake_page_image_bytes(const cake_model_desc* model, int32_t page_tokens) {
     if (!model || page_tokens <= 0) return 0;
     return cake::page_image_bytes(*model, page_tokens);
+}
+
+uint64_t cake_q8_page_bytes(const cake_model_desc* m, int32_t page_tokens, int32_t scale_tokens) {
+    if (!m || m->n_kv_heads <= 0 || (m->head_dim != 64 && m->head_dim != 128)) return 0;
+    if (page_tokens <= 0 || page_tokens % 64 || scale_tokens <= 0 || scale_tokens > 64 || (scale_tokens & (scale_tokens - 1))) return 0;
+    const uint64_t scales = uint64_t(m->n_kv_heads) * uint64_t(page_tokens / scale_tokens);
+    if (scales % 4) return 0;   // every section begins on 16 bytes
+    return 2 * (uint64_t(m->n_kv_heads) * uint64_t(page_tokens) * uint64_t(m->head_dim) + 4 * scales);
+}
+
+int32_t cake_rope_init(cake_rope* out, const cake_rope_desc* d) {
+    if (!out || !d || d->rotary_dim < 2 || d->rotary_dim > 128 || d->rotary_dim % 2) return CAKE_E_INVAL;
+    if (d->layout != CAKE_ROPE_PAIRS && d->layout != CAKE_ROPE_HALVES) return CAKE_E_INVAL;
+    if (d->scaling < CAKE_ROPE_PLAIN || d->scaling > CAKE_ROPE_RAMP || !(d->theta > 1.0) || !std::isfinite(d->theta)) return CAKE_E_INVAL;
+    if (d->scaling != CAKE_ROPE_PLAIN && (!(d->factor >= 1.0) || !std::isfinite(d->factor))) return CAKE_E_INVAL;
+    if (d->scaling >= CAKE_ROPE_BANDS && (!(d->low > 0.0) || !(d->high > d->low) || !std::isfinite(d->high) || d->original_tokens <= 0)) return CAKE_E_INVAL;
+    const double two_pi = 6.283185307179586476925, rd = d->rotary_dim, tokens = d->original_tokens;
+    cake_rope r = {};
+    r.magnitude = 1.0;
+    r.rotary_dim = d->rotary_dim;
+    r.layout = d->layout;
+    double first = 0.0, last = 0.0;   // RAMP: the pairs between which the scaling sets in
+    if (d->scaling == CAKE_ROPE_RAMP) {
+        const auto pair_turning = [&](double times) { return rd * std::log(tokens / (times * two_pi)) / (2.0 * std::log(d->theta)); };
+        first = std::max(std::floor(pair_turning(d->high)), 0.0);
+        last = std::min(std::ceil(pair_turning(d->low)), rd - 1.0);
+        r.magnitude = 0.1 * std::log(d->factor) + 1.0;
+    }
+    for (int i = 0; i < d->rotary_dim / 2; ++i) {
+        const double f = std::pow(d->theta, -2.0 * i / rd);
+        double kept = 1.0;            // share of the unscaled frequency
+        if (d->scaling == CAKE_ROPE_LINEAR) kept = 0.0;
+        else if (d->scaling == CAKE_ROPE_BANDS) kept = (tokens * f / two_pi - d->low) / (d->high - d->low);
+        else if (d->scaling == CAKE_ROPE_RAMP) kept = 1.0 - (i - first) / std::max(last - first, 1e-3);
+        kept = std::min(std::max(kept, 0.0), 1.0);
+        r.freq[i] = d->scaling == CAKE_ROPE_PLAIN ? f : d->scaling == CAKE_ROPE_LINEAR ? f / d->factor : f * kept + f / d->factor * (1.0 - kept);
+    }
+    *out = r;
+    return CAKE_OK;
 }
 
 }  // extern "C"

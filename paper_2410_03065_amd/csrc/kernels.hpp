@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "cake.h"
+
 namespace cake {
 
 typedef __bf16 bf16_t;
@@ -153,5 +155,30 @@ hipError_t launch_decode_attention(int dtype, const float* q, float* out, float*
 constexpr int ARGMAX_BLOCKS = 128;
 struct ArgmaxWs { unsigned long long best[ARGMAX_BLOCKS]; unsigned counter; };
 hipError_t launch_argmax(const float* v, int n, ArgmaxWs* ws, int32_t* result, hipStream_t st);
+
+// ---- a ragged batch over an 8-bit paged cache, one layer (cake_q8_batch) ----
+constexpr int Q8_MOST_TOKENS = 1 << 30;   // a sequence's tokens as the block table can hold them, at most
+struct Q8View {
+    unsigned char* base;                          // the layer's first page
+    const int32_t *table, *seq_len, *row_begin;   // device: [n_seqs][pages_per_seq], [n_seqs], [n_seqs + 1]
+    int n_seqs, pages_per_seq, page_tokens, n_phys, n_kv, head_dim, scale_shift, n_rows;
+    size_t page_bytes, half_bytes, scales_off;    // a page; its K half (V follows); the scales behind a half's codes
+};
+// qkv[n_rows][(n_q + 2 n_kv) hd] -> q[n_q][n_rows][hd] (rotated, dtype), codes and scales of k (rotated) and v in the pages,
+// values[n_rows][2 n_kv][hd] (dtype; null: not) = what the pages then stand for.  max_rows sizes the launch.
+hipError_t launch_append_q8(int dtype, const float* qkv, void* q, void* values, const Q8View& v, const cake_rope& rope, int n_q, int max_rows, hipStream_t st);
+// q[n_q][n_rows][hd] -> out[n_rows][n_q hd]; max_rows and max_len choose kernel and key ranges.
+hipError_t launch_attention_q8(int dtype, const void* q, void* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks,
+                               const AttnWs& ws, hipStream_t st);
+
+// ---- the next token of each row of logits ----
+struct SampleArgs {
+    const float* logits; int64_t row_stride; int rows, vocab;
+    const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p; const float* u;   // [rows]; all but u may be null
+    int32_t* tokens; float* logprobs;                                                                     // logprobs may be null
+};
+constexpr int SAMPLE_MOST_VOCAB = 1 << 19;
+// Takes as many rows at once as the workspace holds (45 KB each; the smallest context has 1.5 MB).
+hipError_t launch_sample(const SampleArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
 
 }  // namespace cake
