@@ -554,7 +554,7 @@ typedef struct {
     int32_t n_seqs;
     int32_t pages_per_seq;
     int32_t page_tokens;        /* a multiple of 64 */
-    int32_t scale_tokens;       /* tokens that share a scale: 1, 2, 4, .. 64; n_kv_heads * page_tokens / scale_tokens a multiple of 4 */
+    int32_t scale_tokens;       /* tokens that share a scale: 1, 4, 8, 16, 32 or 64; n_kv_heads * page_tokens / scale_tokens a multiple of 4 */
     int32_t n_physical_pages;   /* pages per layer in the pool */
     int32_t n_rows;             /* rows of the batch's activations */
     int32_t max_rows;           /* most rows of one sequence and ... */
@@ -606,7 +606,8 @@ int32_t cake_op_append_q8(cake_ctx* ctx, const float* qkv, void* q, void* values
                           const cake_q8_batch* batch);
 /* out[n_rows][n_q * head_dim] = attention of q[n_q][n_rows][head_dim] (both device, model dtype) over layer `layer`: the row at
  * position p sees keys j <= p, with window > 0 only those with p - j < window or j < sinks.  A row that sees no key is zeros.  Scores,
- * softmax and sums in float32; bf16 models round the weights to 16 bits or to 11 (of the largest) on the way into the second product.
+ * softmax and sums in float32; on the way into the second product bf16 models round the weights to 16 bits, or, with more than 32 rows
+ * (n_q / n_kv of them a token), to 11 (and to 2^-33 of the row's largest) and the values to 11.
  * Pointers 16-byte aligned.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
                              const cake_q8_batch* batch);

@@ -137,11 +137,11 @@ def append(pages, qkv, table, lens, begin, n_q, freq, magnitude, layout):
 
 
 def attention(pages, q, table, lens, begin, window=0, sinks=0):
-    """q [n_q][rows][hd] -> (out [rows][n_q][hd], the same with magnitudes of the values, the largest sum of magnitudes of a
-    row's scores), float64.  Rows of no sequence: NaN."""
+    """q [n_q][rows][hd] -> (out [rows][n_q][hd], the same with magnitudes of the values, those magnitudes summed without weights,
+    the largest sum of magnitudes of a row's scores), float64.  Rows of no sequence: NaN."""
     n_q, rows, hd = q.shape
     group = n_q // pages.n_kv
-    out, size, reach = (np.full((rows, n_q, hd), np.nan), np.zeros((rows, n_q, hd)), np.zeros((rows, n_q)))
+    out, size, mass, reach = np.full((rows, n_q, hd), np.nan), np.zeros((rows, n_q, hd)), np.zeros((rows, n_q, hd)), np.zeros((rows, n_q))
     for s in range(len(lens)):
         n = begin[s + 1] - begin[s]
         if n <= 0:
@@ -163,9 +163,10 @@ def attention(pages, q, table, lens, begin, window=0, sinks=0):
                 z = kk @ x / math.sqrt(hd)
                 p = np.exp(z - z.max())
                 p /= p.sum()
-                out[begin[s] + i, h], size[begin[s] + i, h] = p @ vv, p @ np.abs(vv)
-                reach[begin[s] + i, h] = (np.abs(kk) @ np.abs(x)).max() / math.sqrt(hd)
-    return out, size, reach
+                r = begin[s] + i
+                out[r, h], size[r, h], mass[r, h] = p @ vv, p @ np.abs(vv), np.abs(vv).sum(axis=0)
+                reach[r, h] = (np.abs(kk) @ np.abs(x)).max() / math.sqrt(hd)
+    return out, size, mass, reach
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):

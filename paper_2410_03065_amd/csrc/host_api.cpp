@@ -107,7 +107,7 @@ uint64_t cake_page_image_bytes(const cake_model_desc* model, int32_t page_tokens
 
 uint64_t cake_q8_page_bytes(const cake_model_desc* m, int32_t page_tokens, int32_t scale_tokens) {
     if (!m || m->n_kv_heads <= 0 || (m->head_dim != 64 && m->head_dim != 128)) return 0;
-    if (page_tokens <= 0 || page_tokens % 64 || scale_tokens <= 0 || scale_tokens > 64 || (scale_tokens & (scale_tokens - 1))) return 0;
+    if (page_tokens <= 0 || page_tokens % 64 || scale_tokens <= 0 || scale_tokens == 2 || scale_tokens > 64 || (scale_tokens & (scale_tokens - 1))) return 0;
     const uint64_t scales = uint64_t(m->n_kv_heads) * uint64_t(page_tokens / scale_tokens);
     if (scales % 4) return 0;   // every section begins on 16 bytes
     return 2 * (uint64_t(m->n_kv_heads) * uint64_t(page_tokens) * uint64_t(m->head_dim) + 4 * scales);

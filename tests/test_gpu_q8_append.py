@@ -47,7 +47,7 @@ HEADS = [("bf16", 8, 2, 128), ("f32", 4, 4, 64), ("bf16", 12, 4, 64), ("f32", 10
 
 
 @pytest.mark.parametrize("kind,n_q,n_kv,hd", HEADS)
-@pytest.mark.parametrize("block", [1, 2, 16, 64])
+@pytest.mark.parametrize("block", [1, 4, 16, 64])
 @pytest.mark.parametrize("layout", ["pairs", "halves"])
 def test_ragged_batches(kind, n_q, n_kv, hd, block, layout):
     lens, new = [1, 64, 65, 130, 200, 77, 16, 33], [1, 64, 1, 3, 150, 0, 15, 33]

@@ -22,12 +22,12 @@ def test_pages_with_a_scale_per_token_have_the_size_of_a_layer_of_the_int8_store
     lib = cake.load_library()
     image = lib.cake_store_image_bytes(ctypes.byref(cake.model_desc(shape)), pt, cake.STORE_INT8)
     assert cake.q8_page_bytes(shape, pt) * shape.n_layers == image
-    for block in (2, 16, 64):
+    for block in (4, 16, 64):
         pages = serving.Pages(1, shape.n_kv, pt, shape.head_dim, block)
         assert cake.q8_page_bytes(shape, pt, block) == pages.bytes().size
 
 
-@pytest.mark.parametrize("pt,block", [(0, 1), (100, 1), (-64, 1), (64, 0), (64, 3), (64, 128), (64, -1)])
+@pytest.mark.parametrize("pt,block", [(0, 1), (100, 1), (-64, 1), (64, 0), (64, 2), (64, 3), (64, 128), (64, -1)])
 def test_pages_that_are_refused(pt, block):
     with pytest.raises(cake.CakeError):
         cake.q8_page_bytes(si.LLAMA3_8B, pt, block)
