@@ -606,8 +606,9 @@ int32_t cake_op_append_q8(cake_ctx* ctx, const float* qkv, void* q, void* values
                           const cake_q8_batch* batch);
 /* out[n_rows][n_q * head_dim] = attention of q[n_q][n_rows][head_dim] (both device, model dtype) over layer `layer`: the row at
  * position p sees keys j <= p, with window > 0 only those with p - j < window or j < sinks.  A row that sees no key is zeros.  Scores,
- * softmax and sums in float32; on the way into the second product bf16 models round the weights to 16 bits, or, with more than 32 rows
- * (n_q / n_kv of them a token), to 11 (and to 2^-33 of the row's largest) and the values to 11.
+ * softmax and sums in float32; on the way into the second product bf16 models round a weight times its
+ * value's scale to 16 bits, or, with more than 32 rows (n_q / n_kv of them a token), to 11 bits, and to 2^-28 of the row's largest weight times
+ * the largest scale of the key's 64 tokens.
  * Pointers 16-byte aligned.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
                              const cake_q8_batch* batch);

@@ -137,8 +137,8 @@ def append(pages, qkv, table, lens, begin, n_q, freq, magnitude, layout):
 
 
 def attention(pages, q, table, lens, begin, window=0, sinks=0):
-    """q [n_q][rows][hd] -> (out [rows][n_q][hd], the same with magnitudes of the values, those magnitudes summed without weights,
-    the largest sum of magnitudes of a row's scores), float64.  Rows of no sequence: NaN."""
+    """q [n_q][rows][hd] -> (out [rows][n_q][hd], the same with magnitudes of the values, the magnitudes of the codes times the
+    largest scale of their 64 tokens summed without weights, the largest sum of magnitudes of a row's scores), float64.  Rows of no sequence: NaN."""
     n_q, rows, hd = q.shape
     group = n_q // pages.n_kv
     out, size, mass, reach = np.full((rows, n_q, hd), np.nan), np.zeros((rows, n_q, hd)), np.zeros((rows, n_q, hd)), np.zeros((rows, n_q))
@@ -149,6 +149,9 @@ def attention(pages, q, table, lens, begin, window=0, sinks=0):
         used = (max(lens[s], 1) + pages.pt - 1) // pages.pt
         k, v = pages.values(0, table[s, :used], lens[s]), pages.values(1, table[s, :used], lens[s])
         key = np.arange(lens[s])
+        scale = np.repeat(pages.scales[table[s, :used], 1], pages.block, axis=2).transpose(1, 0, 2).reshape(pages.n_kv, -1)[:, :lens[s]].astype(np.float64)
+        pad = np.zeros((pages.n_kv, -lens[s] % 64))
+        most = np.repeat(np.concatenate([scale, pad], axis=1).reshape(pages.n_kv, -1, 64).max(axis=2), 64, axis=1)[:, :lens[s]] if lens[s] else scale
         for i in range(n):
             pos = lens[s] - n + i
             seen = key <= pos
@@ -164,7 +167,7 @@ def attention(pages, q, table, lens, begin, window=0, sinks=0):
                 p = np.exp(z - z.max())
                 p /= p.sum()
                 r = begin[s] + i
-                out[r, h], size[r, h], mass[r, h] = p @ vv, p @ np.abs(vv), np.abs(vv).sum(axis=0)
+                out[r, h], size[r, h], mass[r, h] = p @ vv, p @ np.abs(vv), (np.abs(vv) * (most / scale)[h // group][seen][:, None]).sum(axis=0)
                 reach[r, h] = (np.abs(kk) @ np.abs(x)).max() / math.sqrt(hd)
     return out, size, mass, reach
 

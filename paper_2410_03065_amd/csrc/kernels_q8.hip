@@ -34,6 +34,13 @@ __device__ __forceinline__ float max4(float y) {
     const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+// Maximum over the 16 lanes of a row.
+__device__ __forceinline__ float max16(float y) {
+    y = fmaxf(y, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x121, 0xf, 0xf, false)));   // row_ror:1, 2, 4, 8
+    y = fmaxf(y, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x122, 0xf, 0xf, false)));
+    y = fmaxf(y, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x124, 0xf, 0xf, false)));
+    return fmaxf(y, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x128, 0xf, 0xf, false)));
+}
 __device__ __forceinline__ float sum4(float y) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
     y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
@@ -41,14 +48,18 @@ __device__ __forceinline__ float sum4(float y) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// The batch's arrays are read with uniform indexes and never written by a kernel: through the scalar cache, so that a read
+// waits for no vector load before it.
+__device__ __forceinline__ int uniform(const int32_t* p, size_t i) { return ((const __attribute__((address_space(4))) int32_t*)p)[i]; }
+
 // A sequence of the batch.  What the device arrays say is not trusted: rows stay inside [0, n_rows), and a length that the
 // block table cannot hold (over) is never followed.
 struct Seq { int row0, rows, len; bool over; };
 __device__ __forceinline__ Seq sequence(const Q8View& v, int s) {
     Seq q;
-    q.row0 = min(max(v.row_begin[s], 0), v.n_rows);
-    q.rows = min(max(v.row_begin[s + 1], q.row0), v.n_rows) - q.row0;
-    q.len = min(max(v.seq_len[s], 0), Q8_MOST_TOKENS);
+    q.row0 = min(max(uniform(v.row_begin, s), 0), v.n_rows);
+    q.rows = min(max(uniform(v.row_begin, s + 1), q.row0), v.n_rows) - q.row0;
+    q.len = min(max(uniform(v.seq_len, s), 0), Q8_MOST_TOKENS);
     q.over = q.len > v.pages_per_seq * v.page_tokens;
     return q;
 }
@@ -249,10 +260,12 @@ template <int W> struct KeySteps {
     int sink_steps, first, n;
     __device__ __forceinline__ int at(int i) const { return i < sink_steps ? i : first + i - sink_steps; }
 };
+// Is a key seen by one of the rows at positions lo .. hi?  (window: Q8_MOST_TOKENS where there is none.)
+__device__ __forceinline__ bool visible(int key, int lo, int hi, int window, int sinks) { return (key <= hi) & ((key > lo - window) | (key < sinks)); }
 template <int W> __device__ __forceinline__ KeySteps<W> key_steps(int pos_lo, int pos_hi, int window, int sinks) {
     KeySteps<W> k = {0, 0, 0};
     if (pos_hi < 0) return k;
-    if (window > 0 && pos_lo - window + 1 > 0) {
+    if (pos_lo - window + 1 > 0) {
         k.first = (pos_lo - window + 1) / W;
         k.sink_steps = (min(sinks, pos_lo - window + 1) + W - 1) / W;
         if (k.sink_steps >= k.first) k.first = k.sink_steps = 0;
@@ -335,7 +348,7 @@ attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restr
         auto look_up = [&](int i) {                // a step's physical page, asked for a step ahead of its keys
             const int key0 = ks.at(i) * 32, pg = key0 / v.page_tokens;
             off = key0 - pg * v.page_tokens;
-            phys = v.table[size_t(s) * v.pages_per_seq + pg];
+            phys = uniform(v.table, size_t(s) * v.pages_per_seq + pg);
         };
         auto scales = [&](float (&d)[2][NS], const unsigned char* from) {
             const float* p = (const float*)from;
@@ -373,7 +386,7 @@ attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restr
             const int key0 = ks.at(i) * 32;
             const bool more = i + 4 < c1, was_bad = bad;
             if (more) look_up(i + 4);
-            const bool edge = key0 + 31 > pos_lo || i1 - i0 + 1 < 16 * NB || (window > 0 && key0 <= pos_hi - window && key0 + 31 >= sinks);
+            const bool edge = key0 + 31 > pos_lo || i1 - i0 + 1 < 16 * NB || (key0 <= pos_hi - window && key0 + 31 >= sinks);
             f32x4 sc[NB][2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -402,9 +415,7 @@ attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restr
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + 16 * h + 4 * g4 + e;
-                            const bool seen = key <= pos[r] && (window <= 0 || key > pos[r] - window || key < sinks);
-                            sc[r][h][e] = seen ? sc[r][h][e] : -INFINITY;
+                            sc[r][h][e] = visible(key0 + 16 * h + 4 * g4 + e, pos[r], pos[r], window, sinks) ? sc[r][h][e] : -INFINITY;
                         }
                 }
                 float top = m[r];
@@ -491,27 +502,30 @@ attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restr
     }
 }
 
-// Many rows.  A workgroup takes 32 rows (token, query head of the group) per wave and tiles of 64 keys, which it converts once
-// for all of them on the way into LDS, two tiles there in turn: keys as bfloat16 codes [key][hd], values transposed
-// [hd][key slot] in half precision, code * scale / 2^E.  E is the exponent of the tile's largest scale (kept while it moves by
-// less than 8 times; the outputs are in units of 2^E and move with it), so eleven bits of every value survive whatever the
-// scales' range; scaling the values here saves a multiplication per score.  A value scale that is not finite leaves zeros and
-// a bit in the tile's mask: rows that see its key get a NaN sum, the others nothing.
-// Weights are exp2(score - m) in half precision up to 2^15: m follows a row's maximum only when it would pass that, so the
-// output registers are hardly ever rescaled and rows exchange nothing between lanes on the way.
-// Scores transposed, key slots and the operands' order as above.  Rows of 16 bytes in LDS are swizzled so that neither the
-// 16 rows that a product reads nor those that a conversion writes meet in a bank.
-// Bound by the vector instructions beside the products (8 a score, 2 a code over the workgroup's rows).
+// Many rows.  A workgroup takes 32 rows (token, query head of the group) per wave and tiles of 64 keys, whose codes it converts
+// once for all of them on the way into LDS: keys as bfloat16 [key][hd], values as half precision [hd][key slot], both exact.
+// A weight is exp2(score - m), times its value's scale / 2^E in half precision.  m follows a row's maximum only when a weight
+// would pass 2^11, so the outputs are hardly ever rescaled and rows exchange nothing between lanes on the way.  E is the
+// exponent of the tile's largest scale, kept while it moves by less than 8 times; the outputs are in units of 2^E and move with it.
+// So eleven bits are kept whatever the range of the scales (a single bfloat16, eight bits, would double the output's rounding
+// error), and the largest product stays under 2^15.  A scale that is not finite is left out of the products: it is a bit in the
+// tile's mask, rows that see its key get a NaN sum, and the others nothing.
+// Scores transposed, key slots and the operands' order as above.
+// Bound by the vector instructions beside the products: a score takes 5 and an exponential (four times the issue of one), a
+// code 1.5 over the workgroup's rows.
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
 __device__ __forceinline__ f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ unsigned pack_half(float a, float b) { return __builtin_bit_cast(unsigned, f16x2{_Float16(a), _Float16(b)}); }
 
-constexpr float W_TOP = 15.f, W_FIRST = 8.f;      // largest exponent of a weight; where a row's maximum is put
+// A barrier that waits for LDS alone: the next tiles' loads from memory stay in flight across it.
+__device__ __forceinline__ void phase_end() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+constexpr float W_TOP = 11.f, W_FIRST = 6.f;      // largest exponent of a weight; where a row's maximum is put
 
 template <int HD> struct RowsLds {
     static constexpr int K_BYTES = 64 * HD * 2, TILE = 2 * K_BYTES;
-    static constexpr int KSC = 2 * TILE, INFO = KSC + 2 * 64 * 4, BYTES = INFO + 2 * 16;
+    static constexpr int KSC = 2 * TILE, VSC = KSC + 3 * 64 * 4, INFO = VSC + 3 * 64 * 4, BYTES = INFO + 3 * 16;
 };
 
 template <int HD, int NWV, int NS>
@@ -533,8 +547,13 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
     const bool keys_half = wave < NWV / 2;
     const int st = keys_half ? tid : tid - HALF;              // thread of its half
     const int k_key = st / (HD / CPT), k_at = st % (HD / CPT) * CPT;                          // keys: CPT codes of one key
-    const int v_oct = st / (HD / VC), v_col = st % (HD / VC) * VC;                            // values: VC columns of eight keys
+    const int v_oct = st & 7, v_col = (st >> 3) * VC;                                         // values: VC columns of eight keys
     const int v_key = (v_oct >> 2) * 32 + (v_oct & 3) * 4;                                  // ... v_key + 0..3 and + 16..19
+    // Pieces of 16 bytes in LDS rows: a key's piece p at p ^ key (heads of 64: p ^ key / 2), a column's eight key slots at o ^ column / 2.
+    // 16 rows' pieces of one number lie in different banks then, and a piece's address is one of few bases with an exclusive or.
+    auto k_place = [](int key, int piece) { return key * (HD * 2) + ((piece ^ (HD == 128 ? key & 15 : key >> 1 & 7)) << 4); };
+    auto v_place = [](int col, int oct) { return L::K_BYTES + col * 128 + ((oct ^ (col >> 1 & 7)) << 4); };
+    const int k_put = k_place(k_key, k_at / 8), v_put = v_place(v_col, v_oct), k_get = k_place(n16, g4), v_get = v_place(n16, g4);
 
     for (int tile = tile0; tile * ROWS < n; tile += tiles) {
         const int i0 = tile * ROWS, i1 = min(i0 + ROWS, n) - 1;
@@ -555,7 +574,7 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
             for (int c = 0; c < QC; ++c) qf[r][c] = *(const bf16x8*)(p + 32 * c);
         }
         f32x4 acc[2][HB];
-        float m[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
+        float m[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -564,159 +583,180 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
 
         // ---- a tile's way from memory through registers into LDS
         unsigned raw[CPT / 4];
-        float sc8[2][NS], sc1 = 0.f;
+        float sc1 = 0.f;                                       // key `lane`'s scale, of the key (wave 0) or the value (wave 1)
         bool bad = false;
-        int phys = 0, off = 0, e_now = 0, e_most = -1000;
-        auto look_up = [&](int i) {
-            const int key0 = ks.at(i) * 64, pg = key0 / v.page_tokens;
-            off = key0 - pg * v.page_tokens;
-            phys = v.table[size_t(s) * v.pages_per_seq + pg];
+        int phys = 0, off = -64, pg = 0, e_now = 0, e_most = -1000;
+        auto look_up = [&](int i) {                            // tiles are looked up in their order
+            off += 64;
+            if (off >= v.page_tokens) { off -= v.page_tokens; ++pg; }
+            if (i == c0 || i == ks.sink_steps) { pg = ks.at(i) * 64 / v.page_tokens; off = ks.at(i) * 64 - pg * v.page_tokens; }
+            phys = uniform(v.table, size_t(s) * v.pages_per_seq + pg);
         };
-        auto load = [&] {
+        const unsigned k_from = k_key * HD + k_at, v_from = v_key * HD + v_col;
+        auto load = [&](auto keys_) {
             bad = phys < 0 || phys >= v.n_phys;
-            const unsigned char* page = v.base + size_t(bad ? 0 : phys) * v.page_bytes + (keys_half ? 0 : v.half_bytes);
-            const unsigned char* codes = page + (size_t(g) * v.page_tokens + off) * HD;
-            const float* scales = (const float*)(page + v.scales_off);
-            const int at = g * v.page_tokens + off;
-            if (keys_half) {
+            const unsigned char* page = v.base + size_t(bad ? 0 : phys) * v.page_bytes;
+            const unsigned char* codes = page + (decltype(keys_)::value ? 0 : v.half_bytes) + (size_t(g) * v.page_tokens + off) * HD;
+            if constexpr (decltype(keys_)::value) {
 #pragma unroll
-                for (int c = 0; c < CPT / 16; ++c) *(uint4*)&raw[4 * c] = *(const uint4*)(codes + k_key * HD + k_at + 16 * c);
+                for (int c = 0; c < CPT / 16; ++c) *(uint4*)&raw[4 * c] = *(const uint4*)(codes + k_from + 16 * c);
+                if (wave < 2)
+                    sc1 = ((const float*)(page + wave * v.half_bytes + v.scales_off))[unsigned(g * v.page_tokens + off + lane) >> (NS == 4 ? 0 : v.scale_shift)];
             } else {
 #pragma unroll
                 for (int t = 0; t < 8; ++t) {
-                    const unsigned char* p = codes + (v_key + (t < 4 ? t : t + 12)) * HD + v_col;
+                    const unsigned char* p = codes + v_from + (t < 4 ? t : t + 12) * HD;
                     if constexpr (VC == 8) *(uint2*)&raw[2 * t] = *(const uint2*)p;
                     else if constexpr (VC == 4) raw[t] = *(const unsigned*)p;
                     else raw[t / 2] = t & 1 ? raw[t / 2] | unsigned(*(const unsigned short*)p) << 16 : *(const unsigned short*)p;
                 }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if constexpr (NS == 4) *(float4*)sc8[h] = *(const float4*)(scales + at + v_key + 16 * h);
-                    else sc8[h][0] = scales[(at + v_key + 16 * h) >> v.scale_shift];
-                }
             }
-            sc1 = scales[(at + lane) >> (NS == 4 ? 0 : v.scale_shift)];
         };
-        auto stage = [&](int i, int buf) {
+        auto stage = [&](auto keys_, int c, int buf) {         // piece c of VC: eight keys' elements or a column
             unsigned char* base = lds + buf * L::TILE;
-            const int key0 = ks.at(i) * 64;
-            if (keys_half) {
-#pragma unroll
-                for (int c = 0; c < CPT / 8; ++c) {
-                    const int piece = k_at / 8 + c;
-                    *(bf16x8*)(base + k_key * (HD * 2) + ((piece ^ (k_key & 7)) << 4)) = codes8(raw[2 * c], raw[2 * c + 1]);
-                }
-                if (wave == 0) ((float*)(lds + L::KSC))[buf * 64 + lane] = bad ? __uint_as_float(0x7fc00000u) : sc1 * scale_log2;
+            if constexpr (decltype(keys_)::value) {
+                *(bf16x8*)(base + (k_put ^ (c << 4))) = codes8(raw[2 * c], raw[2 * c + 1]);
             } else {
-                auto seen = [&](int key) { return key <= pos_hi && (window <= 0 || key > pos_lo - window || key < sinks); };
-                const bool mine = seen(key0 + lane), fine = fabsf(sc1) <= FLT_MAX;
-                float top = mine && fine ? sc1 : 0.f;
-                const unsigned long long mask = __builtin_amdgcn_ballot_w64(mine && !fine);
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-                top = max4(top);
-                const unsigned bits = __builtin_amdgcn_readfirstlane(__float_as_uint(top));
+                auto val = [&](int t) {
+                    const unsigned w = VC == 8 ? raw[2 * t + c / 4] : VC == 4 ? raw[t] : raw[t / 2];
+                    return code(w, VC == 2 ? 2 * (t & 1) + c : c & 3);
+                };
+                const uint4 x = {pack_half(val(0), val(1)), pack_half(val(2), val(3)), pack_half(val(4), val(5)), pack_half(val(6), val(7))};
+                *(uint4*)(base + (v_put ^ (c >> 1 << 4)) + c * 128) = x;
+            }
+        };
+        auto stage_scales = [&](int i, int slot) {             // the keys' by the first wave, the values' by the second
+            if (wave == 0) {
+                ((float*)(lds + L::KSC))[slot * 64 + lane] = bad ? __uint_as_float(0x7fc00000u) : sc1 * scale_log2;
+            } else if (wave == 1) {
+                const bool mine = visible(ks.at(i) * 64 + lane, pos_lo, pos_hi, window, sinks), fine = fabsf(sc1) <= FLT_MAX;   // mine: any row's
+                const float x = mine & fine ? sc1 : 0.f;
+                const unsigned long long mask = __builtin_amdgcn_ballot_w64(mine & !fine);
+                const unsigned bits = __builtin_amdgcn_readfirstlane(__float_as_uint(max4(max16(fabsf(x)))));
                 if (bits) {
                     const int e = int(bits >> 23) - 127;
                     e_most = max(e_most, e);
                     if (e > e_now + 3 || e < e_now - 3) e_now = max(e, e_most - 80);
                 }
-                if (wave == NWV / 2 && lane == 0) {
-                    int* info = (int*)(lds + L::INFO + buf * 16);
-                    info[0] = e_now; info[2] = int(unsigned(mask)); info[3] = int(unsigned(mask >> 32));
-                }
-                const float unit = ldexpf(1.f, -e_now);
-                float f[8];
-#pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    const float x = sc8[t / 4][NS == 4 ? t & 3 : 0];
-                    f[t] = seen(key0 + v_key + (t < 4 ? t : t + 12)) && fabsf(x) <= FLT_MAX ? x * unit : 0.f;
-                }
-#pragma unroll
-                for (int j = 0; j < VC; ++j) {
-                    auto val = [&](int t) {
-                        const unsigned w = VC == 8 ? raw[2 * t + j / 4] : VC == 4 ? raw[t] : raw[t / 2];
-                        return code(w, VC == 2 ? 2 * (t & 1) + j : j & 3) * f[t];
-                    };
-                    const uint4 x = {pack_half(val(0), val(1)), pack_half(val(2), val(3)), pack_half(val(4), val(5)), pack_half(val(6), val(7))};
-                    const int row = v_col + j;
-                    *(uint4*)(base + L::K_BYTES + row * 128 + ((v_oct ^ ((row ^ (row >> 3)) & 7)) << 4)) = x;
-                }
+                ((float*)(lds + L::VSC))[slot * 64 + lane] = x * ldexpf(1.f, -e_now);
+                if (lane == 0) *(int4*)(lds + L::INFO + slot * 16) = int4{e_now, 0, int(unsigned(mask)), int(unsigned(mask >> 32))};
             }
         };
-        // ---- a tile's products
-        auto work = [&](int i, int buf) {
-            const int key0 = ks.at(i) * 64;
-            if (key0 > w_hi) return;                                                        // nothing for this wave
-            const bool edge = key0 + 63 > w_lo || w1 - w0 < 31 || (window > 0 && key0 <= w_hi - window && key0 + 63 >= sinks);
-            const unsigned char* kb = lds + buf * L::TILE;
-            const unsigned char* vb = kb + L::K_BYTES;
-            const float* ksc = (const float*)(lds + L::KSC) + buf * 64;
-            const int4 info = *(const int4*)(lds + L::INFO + buf * 16);
-            f32x4 sc[4][2];
+        // ---- a tile's products: scores S^T = K Q^T, and O^T += V^T W^T with the weights of the tile before
+        f32x4 sc[4][2];
+        f16x8 wf[2][2];
+        // An operand read from LDS serves two products.  AHEAD of them are on their way while others are multiplied; the fixed
+        // order keeps the compiler from reading each where it is needed, where it waits for it.
+        auto key_operand = [&](int buf, int x) { return *(const bf16x8*)(lds + buf * L::TILE + (k_get ^ (x % QC << 6)) + x / QC * (16 * HD * 2)); };
+        auto value_operand = [&](int buf, int x) { return *(const bf16x8*)(lds + buf * L::TILE + (v_get ^ ((x & 1) << 6)) + (x >> 1) * 2048); };
+        // between(x): what the vector ALUs do after product x.
+        auto products = [&](auto old_, int old_buf, auto fresh_, int buf, auto between) {
+            constexpr int V = decltype(old_)::value ? 2 * HB : 0, N = V + (decltype(fresh_)::value ? 4 * QC : 0), AHEAD = 8;
+            bf16x8 f[AHEAD];
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) f[x] = x < V ? value_operand(old_buf, x) : key_operand(buf, x - V);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if (x < V) {
+                        acc[r][x >> 1] = mfma16h(__builtin_bit_cast(f16x8, f[x % AHEAD]), wf[r][x & 1], acc[r][x >> 1]);
+                    } else {
+                        f32x4& d = sc[(x - V) / QC][r];
+                        d = mfma16(f[x % AHEAD], qf[r][(x - V) % QC], (x - V) % QC ? d : f32x4{0.f, 0.f, 0.f, 0.f});
+                    }
+                }
+                if (x + AHEAD < N) f[x % AHEAD] = x + AHEAD < V ? value_operand(old_buf, x + AHEAD) : key_operand(buf, x + AHEAD - V);
+                between(x, N);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto unit_of = [&](int e_tile) {      // the outputs in the tile's units
+            if (e_tile == e_acc) return;
+            const float f = ldexpf(1.f, max(e_acc - e_tile, -126));
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int j = 0; j < HB; ++j) acc[r][j] *= f;
+            e_acc = e_tile;
+        };
+        // ---- the weights of a tile from its scores
+        struct Side { float4 ksc[4], vsc[4]; int4 info; };     // what LDS holds beside the operands
+        auto side = [&](int slot) {
+            Side d;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r) sc[h][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < QC; ++c) {
-                    const bf16x8 kf = *(const bf16x8*)(kb + (16 * h + n16) * (HD * 2) + (((c * 4 + g4) ^ (n16 & 7)) << 4));
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) sc[h][r] = mfma16(kf, qf[r][c], sc[h][r]);
-                }
+                d.ksc[h] = *(const float4*)(lds + L::KSC + slot * 256 + 64 * h + 16 * g4);
+                d.vsc[h] = *(const float4*)(lds + L::VSC + slot * 256 + 64 * h + 16 * g4);
             }
-            const int e_tile = __builtin_amdgcn_readfirstlane(info.x);
-            if (e_tile != e_acc) {
-                const float f = ldexpf(1.f, max(e_acc - e_tile, -126));
+            d.info = *(const int4*)(lds + L::INFO + slot * 16);
+            return d;
+        };
+        auto weights = [&](auto first_, int i, const Side& d) {
+            constexpr bool FIRST = decltype(first_)::value;
+            const int key0 = ks.at(i) * 64;
+            const bool odd = __builtin_amdgcn_readfirstlane(d.info.z | d.info.w) != 0;
+            const bool edge = key0 + 63 > w_lo || w1 - w0 < 31 || (key0 <= w_hi - window && key0 + 63 >= sinks);
+            auto seen = [&](int key, int r) { return visible(key, pos[r], pos[r], window, sinks); };
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+            for (int h = 0; h < 4; ++h)
 #pragma unroll
-                    for (int j = 0; j < HB; ++j) acc[r][j] *= f;
-                e_acc = e_tile;
-            }
-            f16x8 wf[2][2];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const float4 k4 = *(const float4*)(ksc + 16 * h + 4 * g4);
-                    sc[h][r][0] *= k4.x; sc[h][r][1] *= k4.y; sc[h][r][2] *= k4.z; sc[h][r][3] *= k4.w;
-                    if (edge)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = key0 + 16 * h + 4 * g4 + e;
-                            const bool seen = key <= pos[r] && (window <= 0 || key > pos[r] - window || key < sinks);
-                            sc[h][r][e] = seen ? sc[h][r][e] : -INFINITY;
-                        }
-                    top = fmaxf(fmaxf(top, fmaxf(sc[h][r][0], sc[h][r][1])), fmaxf(sc[h][r][2], sc[h][r][3]));
+                for (int r = 0; r < 2; ++r) {
+                    sc[h][r][0] = __builtin_fmaf(sc[h][r][0], d.ksc[h].x, -m[r]); sc[h][r][1] = __builtin_fmaf(sc[h][r][1], d.ksc[h].y, -m[r]);
+                    sc[h][r][2] = __builtin_fmaf(sc[h][r][2], d.ksc[h].z, -m[r]); sc[h][r][3] = __builtin_fmaf(sc[h][r][3], d.ksc[h].w, -m[r]);
                 }
-                if (__builtin_amdgcn_ballot_w64(top > m[r] + W_TOP)) {
-                    top = max4(top);
-                    const float to = top > m[r] + W_TOP ? top - W_FIRST : m[r];
-                    const float f = __builtin_amdgcn_exp2f(m[r] - to);
-                    l[r] *= f;
-#pragma unroll
-                    for (int j = 0; j < HB; ++j) acc[r][j] *= f;
-                    m[r] = to;
-                }
+            if (edge) {
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        sc[h][r][e] = __builtin_amdgcn_exp2f(sc[h][r][e] - m[r]);
-                        l[r] += sc[h][r][e];
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[h][r][e] = seen(key0 + 16 * h + 4 * g4 + e, r) ? sc[h][r][e] : -INFINITY;
+            }
+            if (odd) {       // values that are not finite
+                const unsigned long long all = unsigned(d.info.z) | (unsigned long long)unsigned(d.info.w) << 32;
+                for (int k = g4; k < 64; k += 4)
+                    if (all >> k & 1)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) l[r] = seen(key0 + k, r) ? __uint_as_float(0x7fc00000u) : l[r];
+            }
+            float top[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                top[r] = fmaxf(fmaxf(sc[0][r][0], sc[0][r][1]), fmaxf(sc[0][r][2], sc[0][r][3]));
+#pragma unroll
+                for (int h = 1; h < 4; ++h) top[r] = fmaxf(fmaxf(top[r], fmaxf(sc[h][r][0], sc[h][r][1])), fmaxf(sc[h][r][2], sc[h][r][3]));
+            }
+            // a row's reference moves when a weight would pass the largest, and when it sees its first keys
+            auto moves = [&](int r) { return top[r] > W_TOP || (l[r] == 0.f && top[r] > -INFINITY); };
+            if (FIRST || __builtin_amdgcn_ballot_w64(moves(0) || moves(1))) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float t = max4(top[r]);
+                    const float by = t > W_TOP || (sum4(l[r]) == 0.f && t > -INFINITY) ? t - W_FIRST : 0.f, f = FIRST ? 0.f : __builtin_amdgcn_exp2f(-by);
+                    m[r] += by;
+                    if constexpr (!FIRST) {
+                        l[r] *= f;
+#pragma unroll
+                        for (int j = 0; j < HB; ++j) acc[r][j] *= f;
                     }
-                if (info.z | info.w) {      // values that are not finite
-                    const unsigned long long mask = unsigned(info.z) | (unsigned long long)unsigned(info.w) << 32;
 #pragma unroll
                     for (int h = 0; h < 4; ++h)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int k = 16 * h + 4 * g4 + e, key = key0 + k;
-                            const bool seen = key <= pos[r] && (window <= 0 || key > pos[r] - window || key < sinks);
-                            if (seen && (mask >> k & 1)) l[r] = __uint_as_float(0x7fc00000u);
-                        }
+                        for (int e = 0; e < 4; ++e) sc[h][r][e] -= by;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        sc[h][r][e] = __builtin_amdgcn_exp2f(sc[h][r][e]);
+                        l[r] += sc[h][r][e];
+                    }
+                    sc[h][r][0] *= d.vsc[h].x; sc[h][r][1] *= d.vsc[h].y; sc[h][r][2] *= d.vsc[h].z; sc[h][r][3] *= d.vsc[h].w;
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -725,30 +765,62 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                     wf[r][c] = __builtin_bit_cast(f16x8, x);
                 }
             }
-#pragma unroll
-            for (int j = 0; j < HB; ++j)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int row = 16 * j + n16;
-                    const f16x8 vf = *(const f16x8*)(vb + row * 128 + (((c * 4 + g4) ^ ((row ^ (row >> 3)) & 7)) << 4));
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) acc[r][j] = mfma16h(vf, wf[r][c], acc[r][j]);
-                }
         };
-        if (c0 < c1) {
+        // Phases with a barrier between them: the first half of the waves multiplies while the second makes weights, and the other
+        // way round; a SIMD has a wave of each.  In terms of the first half's tile t: phase 2t multiplies values t - 1 and keys t and, between
+        // the products, converts keys t + 1; phase 2t + 1 makes the weights of tile t.  The second half is a phase behind, and
+        // converts values t between its products in phase 2t + 1.  Two buffers of each and three of the scales: all are written a
+        // phase or more after their last reader.
+        const int nt = c1 - c0;
+        auto run = [&](auto keys_) {
+            constexpr bool KEYS = decltype(keys_)::value;
+            constexpr int NEXT = KEYS ? 1 : 0;             // converts tile t + NEXT
+            const std::true_type yes{};
+            const std::false_type no{};
             look_up(c0);
-            load();
-            stage(c0, 0);
-            if (c0 + 1 < c1) { look_up(c0 + 1); load(); }
-            __syncthreads();
-            for (int i = c0; i < c1; ++i) {
-                const int buf = (i - c0) & 1;
-                if (i + 2 < c1) look_up(i + 2);
-                if (i + 1 < c1) stage(i + 1, buf ^ 1);
-                if (i + 2 < c1) load();
-                work(i, buf);
-                __syncthreads();
+            load(keys_);
+            if constexpr (KEYS) {
+#pragma unroll
+                for (int c = 0; c < VC; ++c) stage(keys_, c, 0);
+                stage_scales(c0, 0);
+                if (nt > 1) { look_up(c0 + 1); load(keys_); }
+            } else {
+                phase_end();
             }
+            phase_end();
+            int e_next = 0, slot = 0;                      // slot: t % 3
+            auto phases = [&](auto old, int t) {
+                const int buf = t & 1, after = slot == 2 ? 0 : slot + 1;
+                if (t + NEXT + 1 < nt) look_up(c0 + t + NEXT + 1);
+                products(old, buf ^ 1, yes, buf, [&](int x, int n) {
+                    const int every = (n - 4) / VC;
+                    if (x % every == 0 && x / every < VC) stage(keys_, x / every, KEYS ? buf ^ 1 : buf);
+                    if (x == VC * every) {                 // what was loaded is in LDS: the tile after it
+                        if (KEYS && t + 1 < nt) stage_scales(c0 + t + 1, after);
+                        if (t + NEXT + 1 < nt) load(keys_);
+                    }
+                });
+                phase_end();
+                const Side d = side(slot);
+                __builtin_amdgcn_sched_barrier(0);
+                weights(std::integral_constant<bool, !decltype(old)::value>{}, c0 + t, d);
+                e_next = __builtin_amdgcn_readfirstlane(d.info.x);
+                slot = after;
+                phase_end();
+            };
+            phases(no, 0);
+            for (int t = 1; t < nt; ++t) {
+                unit_of(e_next);
+                phases(yes, t);
+            }
+            unit_of(e_next);
+            products(yes, (nt - 1) & 1, no, 0, [](int, int) {});
+            if (KEYS) phase_end();
+            phase_end();
+        };
+        if (nt > 0) {
+            if (keys_half) run(std::true_type{});
+            else run(std::false_type{});
         }
         const float unit = ldexpf(1.f, e_acc);
 #pragma unroll
@@ -774,7 +846,7 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
 #pragma unroll
                     for (int j = 0; j < HB; ++j)
                         *(float4*)(d + 16 * j + 4 * g4) = make_float4(acc[r][j][0] * unit, acc[r][j][1] * unit, acc[r][j][2] * unit, acc[r][j][3] * unit);
-                if (g4 == 0) { d[HD] = m[r]; d[HD + 1] = sum; }
+                if (g4 == 0) { d[HD] = sum == 0.f ? -FLT_MAX : m[r]; d[HD + 1] = sum; }
             }
         }
     }
@@ -849,7 +921,7 @@ KeyRanges key_ranges(const Q8View& v, int n_q, int rows_per_tile, int width, int
     KeyRanges k;
     const int G = n_q / v.n_kv;
     k.tiles = int(std::min<int64_t>((int64_t(max_rows) * G + rows_per_tile - 1) / rows_per_tile, std::max(1, MOST_GROUPS / (v.n_seqs * v.n_kv))));
-    const int64_t seen = window > 0 ? std::min<int64_t>(max_len, int64_t(window) + sinks + rows_per_tile / G + 2 * width) : max_len;
+    const int64_t seen = std::min<int64_t>(max_len, int64_t(window) + sinks + rows_per_tile / G + 2 * width);
     const int64_t steps = seen / width + 1;
     k.groups = int64_t(v.n_seqs) * v.n_kv * k.tiles;
     int64_t chunk = std::min<int64_t>(std::max<int64_t>(least, (steps * k.groups + want - 1) / want), most);
@@ -908,6 +980,7 @@ hipError_t launch_append_q8(int dtype, const float* qkv, void* q, void* values, 
 hipError_t launch_attention_q8(int dtype, const void* q, void* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks,
                                const AttnWs& ws, hipStream_t st) {
     const int64_t rows = int64_t(max_rows) * (n_q / v.n_kv);
+    window = window == 0 ? Q8_MOST_TOKENS : std::min(window, Q8_MOST_TOKENS);   // none: longer than any sequence, and position - window stays a number
     const float scale = 1.44269504088896340736f / std::sqrt(float(v.head_dim));
     auto go = [&](auto hd, auto ns) {
         constexpr int HD = decltype(hd)::value, NS = decltype(ns)::value;

@@ -52,12 +52,13 @@ class Batch:
 
 def attention_bound(kind, hd, want, size, mass, reach, most_keys):
     """How far an output may be from the exact one.  A score is a float32 sum of head_dim exact products, times a scale: off
-    by at most (hd + 8) 2^-24 of the sum of magnitudes, which changes a weight by a factor e^x.  bf16: a weight keeps 11 bits
-    (off by half a step, 2^-11 of it) and so does a value (2^-11 again), a weight no finer than half a step of 2^-24 where the row's
-    largest is at 2^8 or above, so that each key adds at most 2^-25 / 2^8 of its value, divided by a sum of 1 or more (of the
-    largest).  float32: 24 bits.  Sums of n terms in float32 by 32 keys a step, and half a step of the result's type."""
+    by at most (hd + 8) 2^-24 of the sum of magnitudes, which changes a weight by a factor e^x.  bf16: weight times scale keeps 11
+    bits (off by half a step, 2^-11 of it), but no finer than half a step of 2^-24 in units of which the scale is 2^E and the row's
+    largest weight 2^6 or more; E is the exponent of the largest scale of the key's 64 tokens or up to 3 more.  So each key adds at
+    most 2^-25 2^3 / 2^6 of its code times that largest scale, divided by a sum of 1 or more (of the largest weight).  float32: 24
+    bits.  Sums of n terms in float32 by 32 keys a step, and half a step of the result's type."""
     score = (hd + 8) * 2.0 ** -24 * reach[..., None]
-    weights = 2 * 2.0 ** -11 if kind == "bf16" else 2.0 ** -22
+    weights = 2.0 ** -11 if kind == "bf16" else 2.0 ** -22
     sums = (most_keys / 32 + 64) * 2.0 ** -24
-    floor = 2.0 ** -33 * mass if kind == "bf16" else 0.0
+    floor = 2.0 ** -28 * mass if kind == "bf16" else 0.0
     return (2.0 ** -8 if kind == "bf16" else 2.0 ** -24) * np.abs(want) + size * (2 * np.expm1(score) + weights + sums) + floor + 1e-30
