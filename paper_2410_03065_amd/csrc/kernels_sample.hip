@@ -21,15 +21,30 @@ namespace cake {
 namespace {
 
 typedef unsigned long long u64;
-constexpr int BINS = 1024, LIST = 4096, SLICES = 64;
+constexpr int BINS = 1024, LIST = 4096, SHORT = 512, SLICES = 64;
 constexpr double ONE = 17592186044416.0;          // 2^44, the weight of the likeliest token
 constexpr double BINS_PER_OCTAVE = 22.0;          // 1024 bins over 46 octaves: everything that has a weight
 
+// What the bins say.  Filters end in a bin: top-k in k_bin (none: BINS), top-p, if it alone counts, in p_bin.
+enum Mode {
+    WHOLE,     // no filter cuts anything
+    FRONT,     // the list holds all bins up to `last`, everything that can be kept: SHORT tokens or fewer
+    BIN,       // the list holds bin `last` alone
+    DIGITS     // bin `last` has more than LIST tokens
+};
+struct Plan {
+    Mode mode;
+    bool by_count;            // `last` is where top-k ends (else top-p)
+    int last;
+    unsigned before;          // tokens of the bins before it
+    u64 mass_before, total;   // weight of the bins before it; of all
+};
 struct Row {
     u64 mass[BINS];
     unsigned count[BINS];
-    u64 slice_best[SLICES], slice_mass[SLICES];
+    u64 slice_best[SLICES], part_mass[SLICES * 4];
     unsigned list_n, pad;
+    Plan plan;
     u64 list[LIST];
 };
 
@@ -48,6 +63,26 @@ __device__ __forceinline__ float unorder(unsigned k) { return __uint_as_float(k 
 // (logit, id): larger is earlier in the ranking
 __device__ __forceinline__ u64 rank_key(float l, int id) { return u64(order(l)) << 32 | unsigned(~id); }
 
+// A wave's 64-bit values through its row shifts and broadcasts: lanes without a source get 0.
+template <int CTRL, int ROWS> __device__ __forceinline__ u64 moved(u64 v) {
+    return u64(unsigned(__builtin_amdgcn_update_dpp(0, int(v >> 32), CTRL, ROWS, 0xf, true))) << 32 |
+           unsigned(__builtin_amdgcn_update_dpp(0, int(v), CTRL, ROWS, 0xf, true));
+}
+template <typename F> __device__ __forceinline__ u64 wave_fold(u64 v, F f) {   // inclusive, lane by lane
+    v = f(v, moved<0x111, 0xf>(v));   // row_shr:1, 2, 4, 8
+    v = f(v, moved<0x112, 0xf>(v));
+    v = f(v, moved<0x114, 0xf>(v));
+    v = f(v, moved<0x118, 0xf>(v));
+    v = f(v, moved<0x142, 0xa>(v));   // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+    return f(v, moved<0x143, 0xc>(v));
+}
+__device__ __forceinline__ u64 last_lane(u64 v) {
+    return u64(unsigned(__builtin_amdgcn_readlane(int(v >> 32), 63))) << 32 | unsigned(__builtin_amdgcn_readlane(int(v), 63));
+}
+__device__ __forceinline__ u64 wave_scan(u64 v) { return wave_fold(v, [](u64 a, u64 b) { return a + b; }); }
+__device__ __forceinline__ u64 wave_sum(u64 v) { return last_lane(wave_scan(v)); }
+__device__ __forceinline__ u64 wave_max(u64 v) { return last_lane(wave_fold(v, [](u64 a, u64 b) { return a > b ? a : b; })); }
+
 struct Params {
     float top;          // the row's largest logit
     double octaves;     // log2(e) / T
@@ -58,8 +93,8 @@ struct Params {
 };
 __device__ __forceinline__ Params params(const Args& a, int row) {
     Params r;
-    u64 best = 0;
-    for (int s = 0; s < a.slices; ++s) best = max(best, a.rows[row].slice_best[s]);
+    const int lane = threadIdx.x & 63;
+    const u64 best = wave_max(lane < a.slices ? a.rows[row].slice_best[lane] : 0);
     r.top = unorder(unsigned(best >> 32));
     r.best = unsigned(best >> 32) <= order(-INFINITY) ? -1 : int(~unsigned(best));
     const float t = a.temperature ? a.temperature[row] : 1.f;
@@ -74,40 +109,39 @@ __device__ __forceinline__ Params params(const Args& a, int row) {
     return r;
 }
 
-// The weight, and z in octaves below the top (y <= 0).  2^f on |f| <= 1/2 by its Taylor polynomial in f ln 2: the first term
-// left out is 0.3466^12 / 12! = 6e-15.
-__device__ __forceinline__ u64 weight(float l, const Params& r, double* below = nullptr) {
-    double y = (double(l) - double(r.top)) * r.octaves;
-    if (l == r.top) y = 0.0;                        // also where both are infinite
-    if (below) *below = y;
-    if (!(y > -46.0)) return 0;                     // also NaN
+// z of a token in octaves below the likeliest one's (0 or less); NaN where it can never be chosen.
+__device__ __forceinline__ double octaves(float l, const Params& r) {
+    const double y = (double(l) - double(r.top)) * r.octaves;
+    return l == r.top ? 0.0 : y;                    // also where both are infinite
+}
+__device__ __forceinline__ bool weighs(double y) { return y > -45.0; }
+// Its weight, 1 or more where it weighs.  2^f on |f| <= 1/2 by its Taylor polynomial in f ln 2: the first term left out is
+// 0.3466^12 / 12! = 6e-15.
+__device__ __forceinline__ u64 weight_at(double y) {
+    if (!weighs(y)) return 0;
     const double n = rint(y), f = (y - n) * 0.69314718055994530942;
     double p = 1.0 / 39916800.0;
     p = fma(p, f, 1.0 / 3628800.0); p = fma(p, f, 1.0 / 362880.0); p = fma(p, f, 1.0 / 40320.0); p = fma(p, f, 1.0 / 5040.0);
     p = fma(p, f, 1.0 / 720.0); p = fma(p, f, 1.0 / 120.0); p = fma(p, f, 1.0 / 24.0); p = fma(p, f, 1.0 / 6.0);
     p = fma(p, f, 0.5); p = fma(p, f, 1.0); p = fma(p, f, 1.0);
     // adding 2^52 rounds to a whole number and leaves it in the low bits
-    return u64(__double_as_longlong(ldexp(p, int(n) + 44) + 4503599627370496.0)) & 0xfffffffffffffull;
+    return max(u64(1), u64(__double_as_longlong(ldexp(p, int(n) + 44) + 4503599627370496.0)) & 0xfffffffffffffull);
+}
+__device__ __forceinline__ u64 weight(float l, const Params& r) { return weight_at(octaves(l, r)); }
+
+// The elements of a range, eight loads a thread at a time, of NT threads (64: each wave has a range of its own): f(element, its number).
+template <int NT, typename F> __device__ __forceinline__ void each(const float* l, int lo, int hi, F f) {
+    for (int i = lo + int(threadIdx.x & (NT - 1)); i < hi; i += 8 * NT) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = l[min(i + k * NT, hi - 1)];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i + k * NT < hi) f(x[k], i + k * NT);
+    }
 }
 __device__ __forceinline__ int bin_of(double y) { return min(BINS - 1, int(-y * BINS_PER_OCTAVE)); }
 
-__device__ __forceinline__ u64 shfl_up64(u64 v, int d) {
-    return u64(unsigned(__shfl_up(int(v >> 32), d))) << 32 | unsigned(__shfl_up(int(v), d));
-}
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int d) {
-    return u64(unsigned(__shfl_xor(int(v >> 32), d))) << 32 | unsigned(__shfl_xor(int(v), d));
-}
-__device__ __forceinline__ u64 wave_sum(u64 v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += shfl_xor64(v, d);
-    return v;
-}
-__device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) { const u64 o = shfl_up64(v, d); if (lane >= d) v += o; }
-    return v;
-}
 // Exclusive sums over the workgroup's threads; s: a word per wave.  All threads call it.
 template <int NT> __device__ __forceinline__ u64 block_scan(u64 v, u64* s, u64* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -122,6 +156,12 @@ template <int NT> __device__ __forceinline__ u64 block_scan(u64 v, u64* s, u64* 
     return before + in - v;
 }
 
+// A slice is dealt to its workgroup's four waves in parts: where this thread's (or with next: the one after it) begins.
+__device__ __forceinline__ int part_begin(const Args& a, int slice, int next = 0) {
+    const int lo = slice * a.slice_len, hi = min(a.vocab, lo + a.slice_len);
+    return min(hi, lo + (int(threadIdx.x >> 6) + next) * ((a.slice_len + 3) / 4));
+}
+
 // ---- the largest logit of each slice; the rows' sums cleared
 __global__ void __launch_bounds__(256) sample_max_kernel(Args a) {
     const int row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
@@ -131,10 +171,8 @@ __global__ void __launch_bounds__(256) sample_max_kernel(Args a) {
     const float* l = a.logits + row * a.stride;
     const int lo = slice * a.slice_len, hi = min(a.vocab, lo + a.slice_len);
     u64 best = 0;
-#pragma unroll 4
-    for (int i = lo + threadIdx.x; i < hi; i += 256) best = max(best, rank_key(l[i], i));
-#pragma unroll
-    for (int d = 32; d; d >>= 1) best = max(best, shfl_xor64(best, d));
+    each<256>(l, lo, hi, [&](float x, int i) { best = max(best, rank_key(x, i)); });
+    best = wave_max(best);
     __shared__ u64 s[4];
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = best;
     __syncthreads();
@@ -143,7 +181,7 @@ __global__ void __launch_bounds__(256) sample_max_kernel(Args a) {
 
 // ---- counts and weights by bin, or the slice's weight where no filter needs bins
 __global__ void __launch_bounds__(256) sample_bins_kernel(Args a) {
-    __shared__ u64 mass[BINS], s[4];
+    __shared__ u64 mass[BINS];
     __shared__ unsigned count[BINS];
     const int row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
     const Params p = params(a, row);
@@ -153,41 +191,25 @@ __global__ void __launch_bounds__(256) sample_bins_kernel(Args a) {
     const int lo = slice * a.slice_len, hi = min(a.vocab, lo + a.slice_len);
     if (!p.bins) {
         u64 sum = 0;
-#pragma unroll 4
-        for (int i = lo + threadIdx.x; i < hi; i += 256) { const u64 w = weight(l[i], p); sum += w >= p.least ? w : 0; }
+        each<64>(l, part_begin(a, slice), part_begin(a, slice, 1), [&](float x, int) { const u64 w = weight(x, p); sum += w >= p.least ? w : 0; });
         sum = wave_sum(sum);
-        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) r.slice_mass[slice] = s[0] + s[1] + s[2] + s[3];
+        if ((threadIdx.x & 63) == 0) r.part_mass[slice * 4 + (threadIdx.x >> 6)] = sum;
         return;
     }
     for (int i = threadIdx.x; i < BINS; i += 256) { mass[i] = 0; count[i] = 0; }
     __syncthreads();
-#pragma unroll 4
-    for (int i = lo + threadIdx.x; i < hi; i += 256) {
-        double y;
-        const u64 w = weight(l[i], p, &y);
-        if (w) { atomicAdd(&mass[bin_of(y)], w); atomicAdd(&count[bin_of(y)], 1u); }
-    }
+    const bool masses = p.p < 1.0;     // top-k alone counts
+    each<256>(l, lo, hi, [&](float x, int) {
+        const double y = octaves(x, p);
+        if (!weighs(y)) return;
+        if (masses) atomicAdd(&mass[bin_of(y)], weight_at(y));
+        atomicAdd(&count[bin_of(y)], 1u);
+    });
     __syncthreads();
     for (int i = threadIdx.x; i < BINS; i += 256)
-        if (count[i]) { atomicAdd(&r.mass[i], mass[i]); atomicAdd(&r.count[i], count[i]); }
+        if (count[i]) { if (masses) atomicAdd(&r.mass[i], mass[i]); atomicAdd(&r.count[i], count[i]); }
 }
 
-// What the bins say.  Filters end in a bin: top-k in k_bin (none: BINS), top-p, if it alone counts, in p_bin.
-enum Mode {
-    WHOLE,     // no filter cuts anything
-    FRONT,     // the list holds all bins up to `last`: everything that can be kept
-    BIN,       // the list holds bin `last` alone
-    DIGITS     // bin `last` has more than LIST tokens
-};
-struct Plan {
-    Mode mode;
-    bool by_count;            // `last` is where top-k ends (else top-p)
-    int last;
-    unsigned before;          // tokens of the bins before it
-    u64 mass_before, total;   // weight of the bins before it; of all
-};
 // Finds the bin in which a running count (by_count) or weight reaches `need`: sums before < need <= sums through it.
 template <int NT> __device__ __forceinline__ bool find_bin(const Row& r, bool by_count, double need, u64* s, Plan* shared, Plan* out) {
     constexpr int PER = BINS / NT;
@@ -223,7 +245,7 @@ template <int NT> __device__ __forceinline__ Plan plan(const Row& r, const Param
     }
     if (!cut) { o.mode = WHOLE; o.last = BINS; return o; }
     const unsigned in = r.count[o.last];
-    o.mode = o.before + in <= LIST ? FRONT : in <= LIST ? BIN : DIGITS;
+    o.mode = o.before + in <= SHORT ? FRONT : in <= LIST ? BIN : DIGITS;
     return o;
 }
 
@@ -236,38 +258,38 @@ __global__ void __launch_bounds__(256) sample_gather_kernel(Args a) {
     if (!p.bins) return;
     Row& r = a.rows[row];
     const Plan o = plan<256>(r, p, s, &shared);
+    if (slice == 0 && threadIdx.x == 0) r.plan = o;
     if (o.mode == DIGITS) return;
     const float* l = a.logits + row * a.stride;
-    const int lo = slice * a.slice_len, hi = min(a.vocab, lo + a.slice_len), from = o.mode == FRONT ? 0 : o.last;
+    const int from = o.mode == FRONT ? 0 : o.last;
     u64 sum = 0;
-#pragma unroll 4
-    for (int i = lo + threadIdx.x; i < hi; i += 256) {
-        double y;
-        const float x = l[i];
-        const u64 w = weight(x, p, &y);
-        if (!w) continue;
+    each<64>(l, part_begin(a, slice), part_begin(a, slice, 1), [&](float x, int i) {
+        const double y = octaves(x, p);
+        if (!weighs(y)) return;
         const int b = bin_of(y);
-        if (b < from) sum += w >= p.least ? w : 0;
-        else if (b <= o.last && o.mode != WHOLE) {
+        if (b < from) {
+            const u64 w = weight_at(y);
+            sum += w >= p.least ? w : 0;
+        } else if (b <= o.last && o.mode != WHOLE) {
             const unsigned at = atomicAdd(&r.list_n, 1u);
             if (at < LIST) r.list[at] = rank_key(x, i);
         }
-    }
+    });
     sum = wave_sum(sum);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) r.slice_mass[slice] = s[0] + s[1] + s[2] + s[3];
+    if ((threadIdx.x & 63) == 0) r.part_mass[slice * 4 + (threadIdx.x >> 6)] = sum;
 }
 
 // ---- the row's token
 constexpr int NT = 512, NW = NT / 64;
 
-// Sorts s[0 .. n) (n a power of two) from the largest to the smallest.
+// Sorts s[0 .. n) (n a power of two) from the largest to the smallest.  A wave's pairs of a stage of distance 64 or less lie in
+// 128 elements of its own, and LDS serves a wave in order: only the wider stages need the others.
 __device__ __forceinline__ void sort_down(u64* s, int n) {
+    __syncthreads();
     for (int k = 2; k <= n; k <<= 1)
         for (int j = k >> 1; j; j >>= 1) {
-            __syncthreads();
+            if (j > 64 || (j == 64 && k > 128)) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             for (int i = threadIdx.x; i < n / 2; i += NT) {
                 const int x = (i / j) * 2 * j + i % j, y = x + j;
                 const u64 p = s[x], q = s[y];
@@ -277,14 +299,13 @@ __device__ __forceinline__ void sort_down(u64* s, int n) {
     __syncthreads();
 }
 
-// The first id in [lo, hi) whose running sum of f exceeds `target`; the range's sum has to.  f(id): a whole number.
-template <typename F> __device__ __forceinline__ int first_past(F f, int lo, int hi, u64 target, u64* s, int* found) {
+// The first id in [lo, hi) whose running sum of f exceeds `target`; the range's sum has to.  f(logit, id): a whole number.
+template <typename F> __device__ __forceinline__ int first_past(const float* l, F f, int lo, int hi, u64 target, u64* s, int* found) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     while (hi - lo > 64) {
-        const int seg = (hi - lo + NW - 1) / NW, b = lo + wave * seg, e = min(hi, b + seg);
+        const int seg = (hi - lo + NW - 1) / NW, b = lo + wave * seg;
         u64 sum = 0;
-#pragma unroll 4
-        for (int i = b + lane; i < e; i += 64) sum += f(i);
+        each<64>(l, b, min(hi, b + seg), [&](float x, int i) { sum += f(x, i); });
         sum = wave_sum(sum);
         __syncthreads();
         if (lane == 0) s[wave] = sum;
@@ -296,7 +317,7 @@ template <typename F> __device__ __forceinline__ int first_past(F f, int lo, int
     }
     __syncthreads();
     if (wave == 0) {
-        const u64 v = lo + lane < hi ? f(lo + lane) : 0, in = wave_scan(v);
+        const u64 v = lo + lane < hi ? f(l[lo + lane], lo + lane) : 0, in = wave_scan(v);
         if (in > target && in - v <= target) *found = lo + lane;
     }
     __syncthreads();
@@ -313,15 +334,13 @@ __device__ u64 by_digits(const float* l, int vocab, const Params& p, int last, b
         __syncthreads();
         for (int i = threadIdx.x; i < 256; i += NT) { d_mass[i] = 0; d_count[i] = 0; }
         __syncthreads();
-        for (int i = threadIdx.x; i < vocab; i += NT) {
-            double y;
-            const u64 w = weight(l[i], p, &y);
-            const unsigned k = order(l[i]);
-            if (w && bin_of(y) == last && (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8))) {
-                atomicAdd(&d_mass[k >> shift & 255], w);
-                atomicAdd(&d_count[k >> shift & 255], 1u);
-            }
-        }
+        each<NT>(l, 0, vocab, [&](float x, int) {
+            const double y = octaves(x, p);
+            const unsigned k = order(x);
+            if (!weighs(y) || bin_of(y) != last || (shift < 24 && k >> (shift + 8) != prefix >> (shift + 8))) return;
+            atomicAdd(&d_mass[k >> shift & 255], weight_at(y));
+            atomicAdd(&d_count[k >> shift & 255], 1u);
+        });
         __syncthreads();
         if (threadIdx.x == 0) {
             u64 m = mass, c = count;
@@ -347,15 +366,16 @@ __device__ u64 by_digits(const float* l, int vocab, const Params& p, int last, b
         }
     *kept = mass + ties * w;
     __syncthreads();
-    const int id = first_past([&](int i) -> u64 { return order(l[i]) == prefix; }, 0, vocab, ties - 1, s, found);
+    const int id = first_past(l, [&](float x, int) -> u64 { return order(x) == prefix; }, 0, vocab, ties - 1, s, found);
     return u64(prefix) << 32 | unsigned(~id);
 }
 
 __global__ void __launch_bounds__(NT) sample_pick_kernel(Args a) {
-    __shared__ u64 list[LIST], s[SLICES], d_mass[256];
-    __shared__ unsigned d_count[256], pick;
+    __shared__ u64 list[LIST], s[NW], d_mass[SLICES * 4];     // d_mass: a digit's, then the parts'
+    __shared__ unsigned d_count[256], pick, listed;
     __shared__ Plan shared;
-    __shared__ int found;
+    __shared__ int found, many_kept;
+    __shared__ u64 last_kept;
     const int row = blockIdx.x;
     const Params p = params(a, row);
     if (p.greedy) {
@@ -383,27 +403,28 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(Args a) {
     // the number of the list's first n tokens that are kept when a running weight starting at `mass` may not reach `need`
     // before a token; *kept: the weight through them
     auto ranks_before = [&](int n, u64 mass, double need, u64* kept) {
-        u64 run = mass, total = 0;
-        int many = 0;
+        u64 run = mass;
+        if (threadIdx.x == 0) { last_kept = mass; many_kept = 0; }
         for (int b = 0; b < n; b += NT) {
             const int i = b + int(threadIdx.x);
             const u64 w = i < n ? weight(unorder(unsigned(list[i] >> 32)), p) : 0;
             u64 sum;
             const u64 before = run + block_scan<NT>(w, s, &sum);
-            const bool in = i < n && double(before) < need;
-            u64 wi, ci;
-            block_scan<NT>(in ? w : 0, s, &wi);
-            block_scan<NT>(in, s, &ci);
-            run += sum; total += wi; many += int(ci);
+            run += sum;
+            // the kept are a front: its last one knows their weight
+            if (i < n && double(before) < need && (i == n - 1 || !(double(before + w) < need))) { last_kept = before + w; many_kept = i + 1; }
         }
-        *kept = mass + total;
+        __syncthreads();
+        *kept = last_kept;
+        const int many = many_kept;
+        __syncthreads();
         return many;
     };
     const double none = 1e300;      // a weight that is never reached
 
     u64 least_key = 0;              // kept: rank keys from here on
     bool have_slices = true;
-    const Plan o = p.bins ? plan<NT>(r, p, s, &shared) : Plan{WHOLE, false, BINS, 0, 0, 0};
+    const Plan o = p.bins ? r.plan : Plan{WHOLE, false, BINS, 0, 0, 0};
     if (o.mode == FRONT) {
         int n = int(r.list_n);
         take_list(n);
@@ -475,43 +496,67 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(Args a) {
                 Plan e;
                 find_bin<NT>(r, false, need, s, &shared, &e);
                 u64 got;
-                least_key = by_digits(l, a.vocab, p, e.last, false, need, e.mass_before, s, d_mass, d_count, &pick, &found, &got);
+                if (r.count[e.last] <= LIST) {
+                    if (threadIdx.x == 0) listed = 0;
+                    __syncthreads();
+                    each<NT>(l, 0, a.vocab, [&](float x, int i) {
+                        const double y = octaves(x, p);
+                        if (weighs(y) && bin_of(y) == e.last) list[atomicAdd(&listed, 1u)] = rank_key(x, i);
+                    });
+                    __syncthreads();
+                    n = int(listed);
+                    int up = 2;
+                    while (up < n) up <<= 1;
+                    for (int i = n + int(threadIdx.x); i < up; i += NT) list[i] = 0;
+                    sort_down(list, up);
+                    n = ranks_before(n, e.mass_before, need, &got);
+                    least_key = list[n - 1];
+                } else {
+                    least_key = by_digits(l, a.vocab, p, e.last, false, need, e.mass_before, s, d_mass, d_count, &pick, &found, &got);
+                }
                 have_slices = false;
             }
         }
     }
-    auto weight_of = [&](int i) -> u64 {
-        const u64 w = weight(l[i], p);
-        return w >= p.least && rank_key(l[i], i) >= least_key ? w : 0;
+    auto weight_of = [&](float x, int i) -> u64 {
+        const u64 w = weight(x, p);
+        return w >= p.least && rank_key(x, i) >= least_key ? w : 0;
     };
-    // the slices' weights: known but for the list's tokens, or summed here
+    // the parts' weights: known but for the list's tokens, or summed here
+    const int parts = a.slices * 4, part_len = (a.slice_len + 3) / 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto begin_of = [&](int i) { return min(min(a.vocab, (i / 4 + 1) * a.slice_len), i / 4 * a.slice_len + i % 4 * part_len); };
+    auto end_of = [&](int i) { return min(min(a.vocab, (i / 4 + 1) * a.slice_len), i / 4 * a.slice_len + (i % 4 + 1) * part_len); };
     __syncthreads();
     if (have_slices) {
-        for (int i = threadIdx.x; i < a.slices; i += NT) s[i] = r.slice_mass[i];
+        for (int i = threadIdx.x; i < parts; i += NT) d_mass[i] = r.part_mass[i];
         __syncthreads();
         if (o.mode == BIN)
             for (int i = threadIdx.x; i < int(r.count[o.last]); i += NT) {
                 const u64 k = list[i], w = weight(unorder(unsigned(k >> 32)), p);
-                if (k >= least_key && w >= p.least) atomicAdd(&s[int(~unsigned(k)) / a.slice_len], w);
+                const int id = int(~unsigned(k)), in = id % a.slice_len;
+                if (k >= least_key && w >= p.least) atomicAdd(&d_mass[id / a.slice_len * 4 + in / part_len], w);
             }
     } else {
-        const int lane = threadIdx.x & 63;
-        for (int i = threadIdx.x >> 6; i < a.slices; i += NW) {
-            const int lo = i * a.slice_len, hi = min(a.vocab, lo + a.slice_len);
+        for (int i = wave; i < parts; i += NW) {
             u64 sum = 0;
-            for (int j = lo + lane; j < hi; j += 64) sum += weight_of(j);
+            each<64>(l, begin_of(i), end_of(i), [&](float x, int j) { sum += weight_of(x, j); });
             sum = wave_sum(sum);
-            if (lane == 0) s[i] = sum;
+            if (lane == 0) d_mass[i] = sum;
         }
     }
     __syncthreads();
-    u64 total = 0;
-    for (int i = 0; i < a.slices; ++i) total += s[i];
+    // four parts a lane
+    u64 own[4], mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { own[i] = lane * 4 + i < parts ? d_mass[lane * 4 + i] : 0; mine += own[i]; }
+    const u64 run = wave_scan(mine), total = last_lane(run);
     u64 target = place(total);
-    int slice = 0;
-    for (; slice < a.slices - 1 && target >= s[slice]; ++slice) target -= s[slice];
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(run > target));
+    target -= wave_sum(lane < at ? mine : 0);
+    int part = at * 4;
+    for (; part < at * 4 + 3 && target >= d_mass[part]; ++part) target -= d_mass[part];
     __syncthreads();
-    const int id = first_past(weight_of, slice * a.slice_len, min(a.vocab, (slice + 1) * a.slice_len), target, d_mass, &found);
+    const int id = first_past(l, weight_of, begin_of(part), end_of(part), target, s, &found);
     done(id, total);
 }
 }  // namespace
