@@ -71,184 +71,255 @@ template <> __device__ __forceinline__ bf16_t to_elem<bf16_t>(float x) { return 
 template <typename T, int N> struct Vec { typedef T type __attribute__((__vector_size__(N * sizeof(T)))); };
 
 // ===================================================================================== append
-// Workgroup: `tile` positions of a sequence (a multiple of the block of tokens that shares a scale, aligned to it, so no two
-// workgroups write one block) and one KV head with the query heads of its group.  Sixteen lanes hold a head's row.
-// Bound by the bytes: 4 read per element and 1 or 2 written; the rotation runs in 64 bits (full rate on this chip), because
-// at position 60000 a float32 angle is off by 4e-3 and because the codes that follow are whole numbers: with the rotated
-// value correctly rounded to float32 they do not depend on how cosine and sine were come by.
-template <typename T, int HD>
-__global__ void __launch_bounds__(256)
-append_q8_kernel(const float* __restrict__ qkv, T* __restrict__ q, T* __restrict__ values, Q8View v, cake_rope rope, int n_q, int tile, int tiles) {
-    constexpr int E = HD / 16;                      // elements per lane
-    typedef typename Vec<T, E>::type TV;
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    double2* cs = (double2*)lds;                    // [tile][HD / 2]
-    unsigned* amax = (unsigned*)(lds + size_t(tile) * (HD / 2) * sizeof(double2));   // [K|V][tile]: a block's largest magnitude, then its scale
-    float* ratio = (float*)(amax + 2 * tile);       // [K|V]: what the codes of the first block's older tokens are multiplied by
-    const int g = blockIdx.x % v.n_kv, t_first = blockIdx.x / v.n_kv % tiles, s = blockIdx.x / v.n_kv / tiles;
-    const int G = n_q / v.n_kv, heads = G + 2, all_heads = n_q + 2 * v.n_kv;
-    const int tid = threadIdx.x, group = tid >> 4, e0 = (tid & 15) * E;
-    const Seq seq = sequence(v, s);
-    const int p0 = seq.len - seq.rows, half = rope.rotary_dim / 2, block = 1 << v.scale_shift;
-    const int cap = v.pages_per_seq * v.page_tokens;
-    const int p_new = max(p0, 0), base0 = p_new / tile * tile;   // rows in excess of the sequence's tokens stand for no token
-    const bool pairs = rope.layout == CAKE_ROPE_PAIRS;
+// Cosine and sine of x >= 0 (radians) to some units of 2^-53: x less the nearest multiple of pi / 2, which is subtracted in three
+// parts of 53 bits (the quotient has at most 30), then Taylor polynomials on |r| <= pi / 4, whose first terms left out are
+// 0.785^17 / 17! = 5e-17 and 0.785^18 / 18! = 2e-18.
+__device__ __forceinline__ void turn(double x, double* cosine, double* sine) {
+    const double k = rint(x * 0.63661977236758134308);
+    double r = fma(-k, 1.5707963267948966, x);
+    r = fma(-k, 6.123233995736766e-17, r);
+    r = fma(-k, -1.4973849048591833e-33, r);
+    const double z = r * r;
+    double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+    s = fma(s, z, 1.0 / 6227020800.0); c = fma(c, z, -1.0 / 87178291200.0);
+    s = fma(s, z, -1.0 / 39916800.0);  c = fma(c, z, 1.0 / 479001600.0);
+    s = fma(s, z, 1.0 / 362880.0);     c = fma(c, z, -1.0 / 3628800.0);
+    s = fma(s, z, -1.0 / 5040.0);      c = fma(c, z, 1.0 / 40320.0);
+    s = fma(s, z, 1.0 / 120.0);        c = fma(c, z, -1.0 / 720.0);
+    s = fma(s, z, -1.0 / 6.0);         c = fma(c, z, 1.0 / 24.0);
+    s = fma(s * z, r, r);              c = fma(c, z, -0.5);
+    c = fma(c, z, 1.0);
+    const int quarter = int(k) & 3;
+    const double a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
+    *cosine = quarter == 1 || quarter == 2 ? -a : a;
+    *sine = quarter & 2 ? -b : b;
+}
 
-    for (int t = t_first; base0 + t * tile < seq.len; t += tiles) {
-        const int base = base0 + t * tile;
-        const int lo = max(base, p_new), n = min(base + tile, seq.len) - lo;   // this tile's new positions
+// How a head's elements lie on the 16 lanes that hold it: side by side (adjacent pairs; halves of part of the head, whose
+// partners are read again), or as many of each half where all of the head turns in halves, partners in one lane.
+enum RopeMode { ROPE_ADJACENT, ROPE_HALVES, ROPE_HALVES_PART };
+
+// Two kinds of workgroups.  Rows: eight tokens of a sequence and some of the heads, sixteen heads' rows at a time, four more on
+// their way; with a scale per token that is all.  Blocks, where tokens share scales: 64 positions (whole blocks, aligned, so no
+// two workgroups write one) of one KV head, whose keys and values stay in registers between the largest magnitude and the codes.
+// Bound by the bytes: 4 read per element, 1 or 2 written.  The rotation runs in 64 bits, full rate on this chip: at position 60000
+// a float32 angle is off by 4e-3, and the codes that follow are whole numbers, which with the rotated value correctly rounded to
+// float32 hardly depend on how cosine and sine were come by.
+template <typename T, int HD, int MODE>
+__global__ void __launch_bounds__(256)
+append_q8_kernel(const float* __restrict__ qkv, T* __restrict__ q, T* __restrict__ values, Q8View v, cake_rope rope, int n_q, int row_tiles, int chunks,
+                 int row_groups, int block_tiles) {
+    constexpr int E = HD / 16, P = MODE == ROPE_HALVES ? E / 2 : E, S = MODE == ROPE_HALVES ? HD / 2 : 0;   // elements a lane, in a piece; pieces apart
+    constexpr int TOKENS = 8, AT_ONCE = 4, HELD = 8;
+    typedef typename Vec<float, P < 4 ? P : 4>::type Piece;
+    constexpr int PW = P < 4 ? P : 4;
+    __shared__ double2 cs[TOKENS * (HD / 2)];       // rows: cosine and sine of the tokens' pairs
+    __shared__ unsigned amax[2][64];                // blocks: the largest magnitude, then the scale
+    __shared__ float ratio[2];                      // what the codes of the first block's older tokens are multiplied by
+    const int tid = threadIdx.x, group = tid >> 4, lane = tid & 15, e0 = lane * P;
+    const int half = rope.rotary_dim / 2, block = 1 << v.scale_shift, all_heads = n_q + 2 * v.n_kv;
+    const int cap = v.pages_per_seq * v.page_tokens;
+    auto at = [&](int e) { return e < P ? e0 + e : e0 + S + e - P; };     // the place of a lane's element in its head
+
+    auto read = [&](const float* p, float (&x)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; e += PW) {
+            const Piece w = *(const Piece*)(p + at(e));
+#pragma unroll
+            for (int k = 0; k < PW; ++k) x[e + k] = w[k];
+        }
+    };
+    // rotated in 64 bits, rounded to float32; pair(i): cosine and sine, p: the row (for partners in other lanes)
+    auto rotate = [&](float (&x)[E], auto pair, const float* p) {
+        if constexpr (MODE == ROPE_HALVES) {
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const double2 z = pair(e0 + e);
+                const double a = x[e], b = x[e + P];
+                x[e] = float(a * z.x - b * z.y);
+                x[e + P] = float(a * z.y + b * z.x);
+            }
+        } else if constexpr (MODE == ROPE_ADJACENT) {
+#pragma unroll
+            for (int e = 0; e < E; e += 2)
+                if (e0 + e < rope.rotary_dim) {
+                    const double2 z = pair((e0 + e) / 2);
+                    const double a = x[e], b = x[e + 1];
+                    x[e] = float(a * z.x - b * z.y);
+                    x[e + 1] = float(a * z.y + b * z.x);
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e0 + e < rope.rotary_dim) {
+                    const bool first = e0 + e < half;
+                    const double2 z = pair(first ? e0 + e : e0 + e - half);
+                    const double y = p[first ? e0 + e + half : e0 + e - half];
+                    x[e] = float(first ? double(x[e]) * z.x - y * z.y : double(x[e]) * z.x + y * z.y);
+                }
+        }
+    };
+    auto store = [&](T* d, const float (&x)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; e += P) {
+            typename Vec<T, P>::type o;
+#pragma unroll
+            for (int k = 0; k < P; ++k) o[k] = to_elem<T>(x[e + k]);
+            *(typename Vec<T, P>::type*)(d + at(e)) = o;
+        }
+    };
+    // the row's largest magnitude, as bits: they order like the numbers, and infinities and NaN come out on top
+    auto largest = [&](const float (&x)[E]) {
+        unsigned m = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
+        m = max(m, unsigned(__builtin_amdgcn_update_dpp(0, int(m), 0x121, 0xf, 0xf, false)));   // row_ror:1, 2, 4, 8
+        m = max(m, unsigned(__builtin_amdgcn_update_dpp(0, int(m), 0x122, 0xf, 0xf, false)));
+        m = max(m, unsigned(__builtin_amdgcn_update_dpp(0, int(m), 0x124, 0xf, 0xf, false)));
+        return max(m, unsigned(__builtin_amdgcn_update_dpp(0, int(m), 0x128, 0xf, 0xf, false)));
+    };
+    auto scale_of = [](unsigned m) { return m >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(m) / 127.0f; };
+    auto page_of = [&](int s, int pos) -> unsigned char* {   // null where nothing can be written
+        if (pos >= cap) return nullptr;
+        const int phys = v.table[size_t(s) * v.pages_per_seq + pos / v.page_tokens];
+        return phys < 0 || phys >= v.n_phys ? nullptr : v.base + size_t(phys) * v.page_bytes;
+    };
+    // a token's codes of one head (which: 0 key, 1 value) into its page, and what they stand for
+    auto put = [&](const float (&x)[E], int which, int g, int pos, size_t row, float scale, unsigned char* page) {
+        float c[E];
+        unsigned w[E / P] = {}, wide[E / P] = {};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            c[e] = scale > 0.f ? fminf(fmaxf(rintf(x[e] / scale), -127.f), 127.f) : 0.f;
+            const int k = e % P;
+            (k < 4 ? w : wide)[e / P] |= (unsigned(int(c[e])) & 255u) << (8 * (k & 3));
+        }
+        if (page) {
+            const int off = pos % v.page_tokens;
+            unsigned char* half_page = page + which * v.half_bytes;
+            unsigned char* d = half_page + (size_t(g) * v.page_tokens + off) * HD;
+#pragma unroll
+            for (int k = 0; k < E / P; ++k) {
+                if constexpr (P == 8) *(uint2*)(d + at(k * P)) = uint2{w[k], wide[k]};
+                else if constexpr (P == 4) *(unsigned*)(d + at(k * P)) = w[k];
+                else *(unsigned short*)(d + at(k * P)) = (unsigned short)w[k];
+            }
+            if (block == 1 && lane == 0) ((float*)(half_page + v.scales_off))[size_t(g) * v.page_tokens + off] = scale;
+        }
+        if (values) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) c[e] = page ? c[e] * scale : __uint_as_float(0x7fc00000u);
+            store(values + (row * 2 * v.n_kv + which * v.n_kv + g) * HD, c);
+        }
+    };
+    auto pair_at = [&](int pos, int i) {
+        double2 z;
+        turn(double(pos) * rope.freq[i], &z.x, &z.y);
+        return double2{z.x * rope.magnitude, z.y * rope.magnitude};
+    };
+
+    if (int(blockIdx.x) < row_groups) {
+        // ---- rows
+        int b = blockIdx.x;
+        const int chunk = b % chunks; b /= chunks;
+        const int t0 = b % row_tiles, s = b / row_tiles;
+        const Seq seq = sequence(v, s);
+        const int p0 = seq.len - seq.rows, p_new = max(p0, 0);   // rows in excess of the sequence's tokens stand for no token
+        const int heads = block == 1 ? all_heads : n_q;
+        const int h0 = int(int64_t(heads) * chunk / chunks), nh = int(int64_t(heads) * (chunk + 1) / chunks) - h0;
+        for (int t = t0; p_new + t * TOKENS < seq.len; t += row_tiles) {
+            const int lo = p_new + t * TOKENS, n = min(TOKENS, seq.len - lo), items = n * nh;
+            if (t != t0) __syncthreads();
+            if (h0 < n_q + v.n_kv)
+                for (int i = tid; i < n * half; i += 256) {
+                    const int tok = i / half, f = i - tok * half;
+                    cs[tok * (HD / 2) + f] = pair_at(lo + tok, f);
+                }
+            __syncthreads();
+            for (int i0 = group; i0 < items; i0 += 16 * AT_ONCE) {
+                float x[AT_ONCE][E];
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int i = min(i0 + 16 * k, items - 1), tok = i / nh, h = h0 + i - tok * nh;
+                    read(qkv + (size_t(seq.row0 + lo - p0 + tok) * all_heads + h) * HD, x[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int i = i0 + 16 * k;
+                    if (i >= items) break;
+                    const int tok = i / nh, h = h0 + i - tok * nh, pos = lo + tok;
+                    const size_t row = seq.row0 + lo - p0 + tok;
+                    if (h < n_q + v.n_kv) rotate(x[k], [&](int f) { return cs[tok * (HD / 2) + f]; }, qkv + (row * all_heads + h) * HD);
+                    if (h < n_q) store(q + (size_t(h) * v.n_rows + row) * HD, x[k]);
+                    else put(x[k], h >= n_q + v.n_kv, (h - n_q) % v.n_kv, pos, row, scale_of(largest(x[k])), page_of(s, pos));
+                }
+            }
+        }
+        return;
+    }
+    // ---- blocks
+    int b = blockIdx.x - row_groups;
+    const int g = b % v.n_kv; b /= v.n_kv;
+    const int t0 = b % block_tiles, s = b / block_tiles;
+    const Seq seq = sequence(v, s);
+    const int p0 = seq.len - seq.rows, p_new = max(p0, 0), first = p_new / 64 * 64, blocks = 64 >> v.scale_shift;
+    for (int t = t0; first + t * 64 < seq.len; t += block_tiles) {
+        const int base = first + t * 64, lo = max(base, p_new), n = min(base + 64, seq.len) - lo;
         if (n <= 0) return;
-        if (t != t_first) __syncthreads();
-        for (int i = tid; i < n * half; i += 256) {
-            double sn, cn;
-            sincos(double(lo + i / half) * rope.freq[i % half], &sn, &cn);
-            cs[(i / half) * (HD / 2) + i % half] = double2{cn * rope.magnitude, sn * rope.magnitude};
-        }
-        if (block > 1)
-            for (int i = tid; i < 2 * tile; i += 256) amax[i] = 0;
+        if (t != t0) __syncthreads();
+        float x[HELD][E];
+        auto row_of = [&](int i) { return size_t(seq.row0 + lo - p0 + (i >> 1)); };
+        auto from = [&](int i) { return qkv + (row_of(i) * all_heads + n_q + (i & 1) * v.n_kv + g) * HD; };
+#pragma unroll
+        for (int k = 0; k < HELD; ++k)
+            if (group + 16 * k < 2 * n) read(from(group + 16 * k), x[k]);
+        if (tid < 128) amax[tid >> 6][tid & 63] = 0;
         __syncthreads();
-        // One head's row: rotated (queries and keys) in 64 bits, rounded to float32.
-        auto row_of = [&](int i, int h, float (&x)[E]) {
-            const int row = seq.row0 + (lo + i - p0);
-            const float* p = qkv + (size_t(row) * all_heads + (h < G ? g * G + h : h == G ? n_q + g : n_q + v.n_kv + g)) * HD;
 #pragma unroll
-            for (int e = 0; e < E; e += 4) {
-                const float4 w = *(const float4*)(p + e0 + e);
-                x[e] = w.x; x[e + 1] = w.y; x[e + 2] = w.z; x[e + 3] = w.w;
-            }
-            if (h > G) return;
-            const double2* c = cs + i * (HD / 2);
-            if (pairs) {
-#pragma unroll
-                for (int e = 0; e < E; e += 2)
-                    if (e0 + e < rope.rotary_dim) {
-                        const double2 z = c[(e0 + e) / 2];
-                        const double a = x[e], b = x[e + 1];
-                        x[e] = float(a * z.x - b * z.y);
-                        x[e + 1] = float(a * z.y + b * z.x);
-                    }
-            } else if (e0 < rope.rotary_dim) {
-                float y[E] = {};
-                if (half % E == 0) {            // the partners lie side by side too
-                    const float* o = p + (e0 < half ? e0 + half : e0 - half);
-#pragma unroll
-                    for (int e = 0; e < E; e += 4) {
-                        const float4 w = *(const float4*)(o + e);
-                        y[e] = w.x; y[e + 1] = w.y; y[e + 2] = w.z; y[e + 3] = w.w;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (e0 + e < rope.rotary_dim) y[e] = p[e0 + e < half ? e0 + e + half : e0 + e - half];
-                }
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (e0 + e < rope.rotary_dim) {
-                        const bool first = e0 + e < half;
-                        const double2 z = c[first ? e0 + e : e0 + e - half];
-                        x[e] = float(first ? double(x[e]) * z.x - double(y[e]) * z.y : double(x[e]) * z.x + double(y[e]) * z.y);
-                    }
-            }
-        };
-        // the row's largest magnitude, as bits: they order like the numbers, and infinities and NaN come out on top
-        auto largest = [&](const float (&x)[E]) {
-            unsigned m = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
-#pragma unroll
-            for (int o = 8; o; o >>= 1) m = max(m, unsigned(__shfl_xor(int(m), o, 16)));
-            return m;
-        };
-        auto scale_of = [](unsigned m) { return m >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(m) / 127.0f; };
-        auto page_of = [&](int pos) -> unsigned char* {   // null where nothing can be written
-            if (pos >= cap) return nullptr;
-            const int phys = v.table[size_t(s) * v.pages_per_seq + pos / v.page_tokens];
-            return phys < 0 || phys >= v.n_phys ? nullptr : v.base + size_t(phys) * v.page_bytes;
-        };
-        auto put = [&](int i, int which, const float (&x)[E], float scale, unsigned char* page) {
-            const int pos = lo + i, off = pos % v.page_tokens;
-            float c[E];
-            unsigned w[E / 4] = {};
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                c[e] = scale > 0.f ? fminf(fmaxf(rintf(x[e] / scale), -127.f), 127.f) : 0.f;
-                w[e / 4] |= (unsigned(int(c[e])) & 255u) << (8 * (e & 3));
-            }
-            if (page) {
-                unsigned char* half_page = page + which * v.half_bytes;
-                unsigned* d = (unsigned*)(half_page + (size_t(g) * v.page_tokens + off) * HD + e0);
-#pragma unroll
-                for (int e = 0; e < E / 4; ++e) d[e] = w[e];
-                if (block == 1 && e0 == 0) ((float*)(half_page + v.scales_off))[size_t(g) * v.page_tokens + off] = scale;
-            }
-            if (values) {
-                TV o;
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = to_elem<T>(page ? c[e] * scale : __uint_as_float(0x7fc00000u));
-                *(TV*)(values + (size_t(seq.row0 + pos - p0) * 2 * v.n_kv + which * v.n_kv + g) * HD + e0) = o;
-            }
-        };
-        if (block > 1) {      // a block's scale first: its largest magnitude, over its older tokens' scale too
-            for (int i = group; i < 2 * n; i += 16) {
-                float x[E];
-                const int which = i & 1, tok = i >> 1, pos = lo + tok;
-                row_of(tok, G + which, x);
-                const unsigned a = largest(x);
-                if (e0 == 0) atomicMax(&amax[which * tile + ((pos - base) >> v.scale_shift)], a);
-            }
-            __syncthreads();
-            const int blocks = tile >> v.scale_shift;
-            for (int i = tid; i < 2 * blocks; i += 256) {
-                const int which = i & 1, b = i >> 1, start = base + (b << v.scale_shift);
-                float scale = scale_of(amax[which * tile + b]);
-                unsigned char* page = start < lo + n && start + block > lo ? page_of(start) : nullptr;
-                if (page) {
-                    float* where = (float*)(page + which * v.half_bytes + v.scales_off) +
-                                   ((size_t(g) * v.page_tokens + start % v.page_tokens) >> v.scale_shift);
-                    if (start < lo) {
-                        const float old = *where;
-                        if (!(old <= scale)) scale = old;                 // also where either is NaN
-                        if (amax[which * tile + b] >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);
-                        ratio[which] = scale > 0.f ? old / scale : 1.f;
-                    }
-                    *where = scale;
-                }
-                amax[which * tile + b] = __float_as_uint(scale);
-            }
-            __syncthreads();
-            const int start = lo / block * block;            // the older tokens of the first block
-            if (start < lo) {
-                unsigned char* page = page_of(start);
-                const int words = (lo - start) * (HD / 4);
-                for (int i = tid; page && i < 2 * words; i += 256) {
-                    const int which = i >= words, j = which ? i - words : i;
-                    const float r = ratio[which];
-                    if (!(r < 1.f)) continue;
-                    unsigned* d = (unsigned*)(page + which * v.half_bytes + (size_t(g) * v.page_tokens + start % v.page_tokens) * HD) + j;
-                    const unsigned old = *d;
-                    unsigned w = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) w |= (unsigned(int(fminf(fmaxf(rintf(code(old, k) * r), -127.f), 127.f))) & 255u) << (8 * k);
-                    *d = w;
-                }
-            }
+        for (int k = 0; k < HELD; ++k) {
+            const int i = group + 16 * k;
+            if (i >= 2 * n) break;
+            if (!(i & 1)) rotate(x[k], [&](int f) { return pair_at(lo + (i >> 1), f); }, from(i));
+            const unsigned m = largest(x[k]);
+            if (lane == 0) atomicMax(&amax[i & 1][(lo + (i >> 1) - base) >> v.scale_shift], m);
         }
-        for (int i = group; i < n * heads; i += 16) {
-            const int tok = i / heads, h = i - tok * heads, pos = lo + tok;
-            float x[E];
-            row_of(tok, h, x);
-            if (h < G) {
-                TV o;
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = to_elem<T>(x[e]);
-                *(TV*)(q + (size_t(g * G + h) * v.n_rows + seq.row0 + pos - p0) * HD + e0) = o;
-            } else {
-                const int which = h - G;
-                float scale;
-                if (block > 1) scale = __uint_as_float(amax[which * tile + ((pos - base) >> v.scale_shift)]);
-                else scale = scale_of(largest(x));
-                put(tok, which, x, scale, page_of(pos));
+        __syncthreads();
+        unsigned char* const page = page_of(s, base);               // 64 positions lie in one page
+        if (tid < 2 * blocks) {
+            const int which = tid & 1, k = tid >> 1, start = base + (k << v.scale_shift);
+            const unsigned m = amax[which][k];
+            float scale = scale_of(m);
+            if (page && start < lo + n && start + block > lo) {
+                float* where = (float*)(page + which * v.half_bytes + v.scales_off) + ((size_t(g) * v.page_tokens + start % v.page_tokens) >> v.scale_shift);
+                if (start < lo) {                                    // the block holds older tokens
+                    const float old = *where;
+                    if (!(old <= scale)) scale = old;                 // also where either is NaN
+                    if (m >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);
+                    ratio[which] = scale > 0.f ? old / scale : 1.f;
+                }
+                *where = scale;
             }
+            amax[which][k] = __float_as_uint(scale);
+        }
+        __syncthreads();
+        const int start = lo / block * block, words = (lo - start) * (HD / 4);   // the older tokens of the first block
+        for (int i = tid; page && i < 2 * words; i += 256) {
+            const int which = i >= words, j = which ? i - words : i;
+            const float r = ratio[which];
+            if (!(r < 1.f)) continue;
+            unsigned* d = (unsigned*)(page + which * v.half_bytes + (size_t(g) * v.page_tokens + start % v.page_tokens) * HD) + j;
+            const unsigned old = *d;
+            unsigned w = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w |= (unsigned(int(fminf(fmaxf(rintf(code(old, k) * r), -127.f), 127.f))) & 255u) << (8 * k);
+            *d = w;
+        }
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            const int i = group + 16 * k;
+            if (i >= 2 * n) break;
+            const int pos = lo + (i >> 1);
+            put(x[k], i & 1, g, pos, row_of(i), __uint_as_float(amax[i & 1][(pos - base) >> v.scale_shift]), page);
         }
     }
 }
@@ -904,14 +975,19 @@ constexpr int MOST_GROUPS = 1 << 18;
 
 template <typename T, int HD>
 hipError_t append_q8(const float* qkv, T* q, T* values, const Q8View& v, const cake_rope& rope, int n_q, int max_rows, hipStream_t st) {
-    const int tile = std::max(16, 1 << v.scale_shift), tiles = std::min((max_rows + tile - 1) / tile + 1, std::max(1, MOST_GROUPS / (v.n_seqs * v.n_kv)));
-    const size_t lds = size_t(tile) * (HD / 2) * sizeof(double2) + (2 * tile + 2) * 4;
-    if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void*)append_q8_kernel<T, HD>, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((append_q8_kernel<T, HD>), dim3(unsigned(size_t(v.n_seqs) * tiles * v.n_kv)), dim3(256), lds, st, qkv, q, values, v, rope, n_q, tile, tiles);
-    return hipGetLastError();
+    const int most = std::max(1, MOST_GROUPS / (v.n_seqs * v.n_kv)), heads = v.scale_shift ? n_q : n_q + 2 * v.n_kv;
+    const int row_tiles = std::min((max_rows + 7) / 8, most), block_tiles = v.scale_shift ? std::min((max_rows + 63) / 64 + 1, most) : 0;
+    // few rows: their heads on several workgroups, down to one row of a head per sixteen lanes
+    const int chunks = std::max(1, std::min((heads * std::min(max_rows, 8) + 15) / 16, 1024 / (v.n_seqs * row_tiles)));
+    const int row_groups = v.n_seqs * row_tiles * chunks, block_groups = v.n_seqs * block_tiles * v.n_kv;
+    auto go = [&](auto mode) {
+        hipLaunchKernelGGL((append_q8_kernel<T, HD, decltype(mode)::value>), dim3(unsigned(row_groups + block_groups)), dim3(256), 0, st, qkv, q, values, v, rope,
+                           n_q, row_tiles, chunks, row_groups, block_tiles);
+        return hipGetLastError();
+    };
+    if (rope.layout == CAKE_ROPE_PAIRS) return go(std::integral_constant<int, ROPE_ADJACENT>{});
+    if (rope.rotary_dim == HD) return go(std::integral_constant<int, ROPE_HALVES>{});
+    return go(std::integral_constant<int, ROPE_HALVES_PART>{});
 }
 
 // How a launch divides the keys: `chunk` steps of `width` keys to a workgroup, at most `splits` ranges.
