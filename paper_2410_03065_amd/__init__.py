@@ -357,6 +357,8 @@ class Engine:
         self.page_tokens = page_tokens
         self.max_tokens, self.max_chunk = max_tokens, max_chunk
         self._take_streams(compute_stream)
+        self._dev_index = self.dev.index if self.dev.index is not None else torch.cuda.current_device()
+        self._compute_raw = self.compute_stream.cuda_stream
         self._tensors = []
         self.with_head = with_head or (weights is not None and "lm_head" in weights)
         self._build_weights(weights, seed)
@@ -807,20 +809,21 @@ class Engine:
         return out
 
     # -- a ragged batch over an 8-bit cache ---------------------------------------------
-    def _in_order(self, call, what):
+    def _in_order(self, fn, what, *args):
         """A call whose work is to run between what torch's current stream has and what it gets next."""
-        current = self.torch.cuda.current_stream(self.dev)
-        same = current.cuda_stream == self.compute_stream.cuda_stream
-        if not same:
+        if self.torch._C._cuda_getCurrentRawStream(self._dev_index) == self._compute_raw:
+            rc = fn(self.ctx, *args)
+        else:
+            current = self.torch.cuda.current_stream(self.dev)
             self.compute_stream.wait_stream(current)
-        rc = call()
-        if not same:
+            rc = fn(self.ctx, *args)
             current.wait_stream(self.compute_stream)
-        self._check(rc, what)
+        if rc != OK:
+            self._check(rc, what)
 
     def _operand(self, t, name, dtype, shape=None):
         """Address of a contiguous tensor on the engine's device, or a refusal."""
-        if t.dtype != dtype or t.device != self.dev or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        if t.dtype is not dtype or t.get_device() != self._dev_index or not t.is_contiguous() or (shape is not None and t.shape != shape):
             raise CakeError(E_INVAL, "%s: a contiguous %s tensor%s on %s is needed, got %s %s on %s" % (
                 name, dtype, "" if shape is None else " of %s" % (tuple(shape),), self.dev, t.dtype, tuple(t.shape), t.device))
         return t.data_ptr()
@@ -854,9 +857,9 @@ class Engine:
         if q is None:
             q = self.torch.empty((s.n_q, n, s.head_dim), dtype=self.tdtype, device=self.dev)
         values = self.torch.empty((n, 2 * s.n_kv, s.head_dim), dtype=self.tdtype, device=self.dev) if want_values else None
-        args = (self._operand(qkv, "qkv", self.torch.float32, (n, (s.n_q + 2 * s.n_kv) * s.head_dim)),
-                self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)), values.data_ptr() if want_values else None)
-        self._in_order(lambda: self.lib.cake_op_append_q8(self.ctx, *args, layer, C.byref(rope), C.byref(batch)), "cake_op_append_q8")
+        self._in_order(self.lib.cake_op_append_q8, "cake_op_append_q8",
+                       self._operand(qkv, "qkv", self.torch.float32, (n, (s.n_q + 2 * s.n_kv) * s.head_dim)),
+                       self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)), values.data_ptr() if want_values else None, layer, rope, batch)
         return (q, values) if want_values else q
 
     def op_attention_q8(self, q, layer, batch, window=0, sinks=0, out=None):
@@ -864,25 +867,27 @@ class Engine:
         s, n = self.shape, batch.n_rows
         if out is None:
             out = self.torch.empty((n, s.n_q * s.head_dim), dtype=self.tdtype, device=self.dev)
-        args = (self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)), self._operand(out, "out", self.tdtype, (n, s.n_q * s.head_dim)))
-        self._in_order(lambda: self.lib.cake_op_attention_q8(self.ctx, *args, layer, window, sinks, C.byref(batch)), "cake_op_attention_q8")
+        self._in_order(self.lib.cake_op_attention_q8, "cake_op_attention_q8", self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)),
+                       self._operand(out, "out", self.tdtype, (n, s.n_q * s.head_dim)), layer, window, sinks, batch)
         return out
 
     def op_sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
         """The next token of each row of logits (float32 [rows][vocab], rows any distance apart) and its log-probability; u and the
         settings are tensors of a value per row (cake_op_sample)."""
         torch = self.torch
-        if logits.dim() != 2 or logits.dtype != torch.float32 or logits.device != self.dev or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        if logits.dim() != 2 or logits.dtype is not torch.float32 or logits.get_device() != self._dev_index or (logits.shape[1] > 1 and logits.stride(1) != 1):
             raise CakeError(E_INVAL, "op_sample: logits must be float32 [rows][vocab] on %s with neighbouring elements side by side" % self.dev)
         rows, vocab = logits.shape
         tokens = torch.empty(rows, dtype=torch.int32, device=self.dev)
         logprobs = torch.empty(rows, dtype=torch.float32, device=self.dev)
-        a = [None if t is None else self._operand(t, n, d, (rows,)) for t, n, d in (
-            (temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
-            (min_p, "min_p", torch.float32), (u, "u", torch.float32))]
+        f32, one = torch.float32, (rows,)
         stride = logits.stride(0) if rows > 1 else max(logits.stride(0), vocab)
-        self._in_order(lambda: self.lib.cake_op_sample(self.ctx, logits.data_ptr(), stride, rows, vocab, *a, tokens.data_ptr(),
-                                                       logprobs.data_ptr()), "cake_op_sample")
+        self._in_order(self.lib.cake_op_sample, "cake_op_sample", logits.data_ptr(), stride, rows, vocab,
+                       None if temperature is None else self._operand(temperature, "temperature", f32, one),
+                       None if top_k is None else self._operand(top_k, "top_k", torch.int32, one),
+                       None if top_p is None else self._operand(top_p, "top_p", f32, one),
+                       None if min_p is None else self._operand(min_p, "min_p", f32, one),
+                       self._operand(u, "u", f32, one), tokens.data_ptr(), logprobs.data_ptr())
         return tokens, logprobs
 
     def close(self):

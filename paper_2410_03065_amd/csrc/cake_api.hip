@@ -1544,6 +1544,15 @@ int32_t cake_op_decode_attention_static(cake_ctx* c, const float* q, float* out,
 }
 
 // ---- a ragged batch over an 8-bit cache ---------------------------------------------------
+// The context's device as the current one while a call lasts (its streams and memory belong to it).
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(int device) {
+        int now = device;
+        if (hipGetDevice(&now) == hipSuccess && now != device && hipSetDevice(device) == hipSuccess) before = now;
+    }
+    ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
 static bool off16(const void* p) { return (uintptr_t(p) & 15) != 0; }
 
 // Checks what the host can see of a batch (its arrays are read on the device) and lays out the view of one layer.
@@ -1581,6 +1590,7 @@ int32_t cake_op_append_q8(cake_ctx* c, const float* qkv, void* q, void* values, 
         return fail(c, CAKE_E_INVAL, "op_append_q8: rotary description: null, or not for heads of %d", c->m.head_dim);
     if (v.n_rows == 0 || v.n_seqs == 0) return CAKE_OK;
     if (!qkv || !q || off16(qkv) || off16(q) || off16(values)) return fail(c, CAKE_E_INVAL, "op_append_q8: qkv, q or values null or not 16-byte aligned");
+    const OnDevice on(c->device);
     HIP_TRY(c, launch_append_q8(c->m.dtype, qkv, q, values, v, *rope, c->m.n_q_heads, max_rows, c->cs));
     return CAKE_OK;
 }
@@ -1594,6 +1604,7 @@ int32_t cake_op_attention_q8(cake_ctx* c, const void* q, void* out, int32_t laye
     if (window < 0 || sinks < 0) return fail(c, CAKE_E_INVAL, "op_attention_q8: window %d, sinks %d", window, sinks);
     if (v.n_rows == 0 || v.n_seqs == 0) return CAKE_OK;
     if (!q || !out || off16(q) || off16(out)) return fail(c, CAKE_E_INVAL, "op_attention_q8: q or out null or not 16-byte aligned");
+    const OnDevice on(c->device);
     HIP_TRY(c, launch_attention_q8(c->m.dtype, q, out, v, c->m.n_q_heads, max_rows, max_len, window, sinks, AttnWs{c->split.part, c->split.part_bytes, 0}, c->cs));
     return CAKE_OK;
 }
@@ -1605,6 +1616,7 @@ int32_t cake_op_sample(cake_ctx* c, const float* logits, int64_t row_stride, int
         return fail(c, CAKE_E_INVAL, "op_sample: %d rows of %d logits, %lld apart", rows, vocab, (long long)row_stride);
     if (rows == 0) return CAKE_OK;
     if (!logits || !u || !tokens) return fail(c, CAKE_E_INVAL, "op_sample: null pointer");
+    const OnDevice on(c->device);
     HIP_TRY(c, launch_sample({logits, row_stride, rows, vocab, temperature, top_k, top_p, min_p, u, tokens, logprobs}, c->split.part, c->split.part_bytes, c->cs));
     return CAKE_OK;
 }

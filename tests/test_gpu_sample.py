@@ -31,7 +31,7 @@ def check(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, devic
     fine = np.isfinite(want_lp)
     np.testing.assert_array_equal(lp[~fine], want_lp[~fine])
     # one rounding to float32 of a number computed in 64 bits; weights are whole multiples of 2^-44, so a sum of n is off by n 2^-45
-    assert (np.abs(lp - want_lp)[fine] <= 2.0 ** -24 * np.abs(want_lp[fine]) + 1e-7).all()
+    assert (np.abs(lp[fine] - want_lp[fine]) <= 2.0 ** -24 * np.abs(want_lp[fine]) + 1e-7).all()
     return want
 
 
