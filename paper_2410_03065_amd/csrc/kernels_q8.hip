@@ -589,6 +589,9 @@ typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
 __device__ __forceinline__ f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ unsigned pack_half(float a, float b) { return __builtin_bit_cast(unsigned, f16x2{_Float16(a), _Float16(b)}); }
 
+// Of whole numbers up to 127, which need no rounding: one instruction a pair.
+__device__ __forceinline__ unsigned pack_code(float a, float b) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(a, b)); }
+
 // A barrier that waits for LDS alone: the next tiles' loads from memory stay in flight across it.
 __device__ __forceinline__ void phase_end() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -692,7 +695,7 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                     const unsigned w = VC == 8 ? raw[2 * t + c / 4] : VC == 4 ? raw[t] : raw[t / 2];
                     return code(w, VC == 2 ? 2 * (t & 1) + c : c & 3);
                 };
-                const uint4 x = {pack_half(val(0), val(1)), pack_half(val(2), val(3)), pack_half(val(4), val(5)), pack_half(val(6), val(7))};
+                const uint4 x = {pack_code(val(0), val(1)), pack_code(val(2), val(3)), pack_code(val(4), val(5)), pack_code(val(6), val(7))};
                 *(uint4*)(base + (v_put ^ (c >> 1 << 4)) + c * 128) = x;
             }
         };
@@ -718,27 +721,41 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
         f16x8 wf[2][2];
         // An operand read from LDS serves two products.  AHEAD of them are on their way while others are multiplied; the fixed
         // order keeps the compiler from reading each where it is needed, where it waits for it.
-        auto key_operand = [&](int buf, int x) { return *(const bf16x8*)(lds + buf * L::TILE + (k_get ^ (x % QC << 6)) + x / QC * (16 * HD * 2)); };
-        auto value_operand = [&](int buf, int x) { return *(const bf16x8*)(lds + buf * L::TILE + (v_get ^ ((x & 1) << 6)) + (x >> 1) * 2048); };
-        // between(x): what the vector ALUs do after product x.
-        auto products = [&](auto old_, int old_buf, auto fresh_, int buf, auto between) {
-            constexpr int V = decltype(old_)::value ? 2 * HB : 0, N = V + (decltype(fresh_)::value ? 4 * QC : 0), AHEAD = 8;
-            bf16x8 f[AHEAD];
+        // Two chains of sums side by side, each for both blocks of rows: four products between a sum's next.
+        auto key_block = [](int x) { return x / (2 * QC) * 2 + (x & 1); };
+        auto key_part = [](int x) { return (x >> 1) % QC; };
+        auto value_block = [](int x) { return (x >> 2) * 2 + (x & 1); };
+        auto value_part = [](int x) { return (x >> 1) & 1; };
+        auto key_operand = [&](int buf, int x) { return *(const bf16x8*)(lds + buf * L::TILE + (k_get ^ (key_part(x) << 6)) + key_block(x) * (16 * HD * 2)); };
+        auto value_operand = [&](int buf, int x) { return *(const bf16x8*)(lds + buf * L::TILE + (v_get ^ (value_part(x) << 6)) + value_block(x) * 2048); };
+        // The scores' come first: theirs are asked for before the phase begins (early).  between(x): what the vector ALUs do after
+        // product x.
+        constexpr int AHEAD = 4;
+        bf16x8 f[AHEAD];
+        auto early = [&](int buf) {
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x) f[x] = x < V ? value_operand(old_buf, x) : key_operand(buf, x - V);
+            for (int x = 0; x < AHEAD; ++x) f[x] = key_operand(buf, x);
+        };
+        auto products = [&](auto fresh_, int buf, auto old_, int old_buf, auto between) {
+            constexpr int K = decltype(fresh_)::value ? 4 * QC : 0, N = K + (decltype(old_)::value ? 2 * HB : 0);
+            auto operand = [&](int x) { return x < K ? key_operand(buf, x) : value_operand(old_buf, x - K); };
+            if constexpr (K == 0)
+#pragma unroll
+                for (int x = 0; x < AHEAD; ++x) f[x] = operand(x);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int x = 0; x < N; ++x) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    if (x < V) {
-                        acc[r][x >> 1] = mfma16h(__builtin_bit_cast(f16x8, f[x % AHEAD]), wf[r][x & 1], acc[r][x >> 1]);
+                    if (x < K) {
+                        f32x4& d = sc[key_block(x)][r];
+                        d = mfma16(f[x % AHEAD], qf[r][key_part(x)], key_part(x) ? d : f32x4{0.f, 0.f, 0.f, 0.f});
                     } else {
-                        f32x4& d = sc[(x - V) / QC][r];
-                        d = mfma16(f[x % AHEAD], qf[r][(x - V) % QC], (x - V) % QC ? d : f32x4{0.f, 0.f, 0.f, 0.f});
+                        f32x4& d = acc[r][value_block(x - K)];
+                        d = mfma16h(__builtin_bit_cast(f16x8, f[x % AHEAD]), wf[r][value_part(x - K)], d);
                     }
                 }
-                if (x + AHEAD < N) f[x % AHEAD] = x + AHEAD < V ? value_operand(old_buf, x + AHEAD) : key_operand(buf, x + AHEAD - V);
+                if (x + AHEAD < N) f[x % AHEAD] = operand(x + AHEAD);
                 between(x, N);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -855,37 +872,39 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                 for (int c = 0; c < VC; ++c) stage(keys_, c, 0);
                 stage_scales(c0, 0);
                 if (nt > 1) { look_up(c0 + 1); load(keys_); }
+                if (nt > 2) look_up(c0 + 2);
             } else {
+                if (nt > 1) look_up(c0 + 1);
                 phase_end();
             }
             phase_end();
             int e_next = 0, slot = 0;                      // slot: t % 3
             auto phases = [&](auto old, int t) {
                 const int buf = t & 1, after = slot == 2 ? 0 : slot + 1;
-                if (t + NEXT + 1 < nt) look_up(c0 + t + NEXT + 1);
-                products(old, buf ^ 1, yes, buf, [&](int x, int n) {
-                    const int every = (n - 4) / VC;
-                    if (x % every == 0 && x / every < VC) stage(keys_, x / every, KEYS ? buf ^ 1 : buf);
-                    if (x == VC * every) {                 // what was loaded is in LDS: the tile after it
-                        if (KEYS && t + 1 < nt) stage_scales(c0 + t + 1, after);
-                        if (t + NEXT + 1 < nt) load(keys_);
-                    }
+                products(yes, buf, old, buf ^ 1, [&](int x, int n) {
+                    const int every = n / 2 / VC, c = (x - n / 2) / every;      // from half way on: the loads are a phase old
+                    if (x >= n / 2 && (x - n / 2) % every == 0 && c < VC) stage(keys_, c, KEYS ? buf ^ 1 : buf);
                 });
                 phase_end();
+                if (KEYS && t + 1 < nt) stage_scales(c0 + t + 1, after);
+                if (t + NEXT + 1 < nt) load(keys_);        // what was loaded is in LDS: the tile after it,
+                if (t + NEXT + 2 < nt) look_up(c0 + t + NEXT + 2);   // and where the next one is
                 const Side d = side(slot);
                 __builtin_amdgcn_sched_barrier(0);
                 weights(std::integral_constant<bool, !decltype(old)::value>{}, c0 + t, d);
                 e_next = __builtin_amdgcn_readfirstlane(d.info.x);
                 slot = after;
+                if (t + 1 < nt) early(buf ^ 1);
                 phase_end();
             };
+            early(0);
             phases(no, 0);
             for (int t = 1; t < nt; ++t) {
                 unit_of(e_next);
                 phases(yes, t);
             }
             unit_of(e_next);
-            products(yes, (nt - 1) & 1, no, 0, [](int, int) {});
+            products(no, 0, yes, (nt - 1) & 1, [](int, int) {});
             if (KEYS) phase_end();
             phase_end();
         };
