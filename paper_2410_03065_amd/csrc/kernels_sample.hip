@@ -50,10 +50,15 @@ struct Row {
 };
 
 struct Args {
-    const float* logits; int64_t stride; int vocab, slices, slice_len;
+    const float* logits; int64_t stride; int rows_n, vocab, slices, slice_len;
     const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p; const float* u;
     int32_t* tokens; float* logprobs; Row* rows;
 };
+
+// Workgroups go round the eight XCDs; their numbers go to runs of neighbours on each, so that a row's slices share one L2 with their
+// sums and, from the second kernel on, their logits.  The grid: n rounded up to 8.
+__device__ __forceinline__ int xcd_order(int n) { return int(blockIdx.x & 7) * ((n + 7) / 8) + int(blockIdx.x >> 3); }
+inline unsigned xcd_grid(int n) { return unsigned((n + 7) / 8 * 8); }
 
 // Float bits that order like the numbers; 0 for what can never be chosen (NaN).  -0 counts as 0.
 __device__ __forceinline__ unsigned order(float l) {
@@ -179,7 +184,8 @@ __device__ __forceinline__ int part_begin(const Args& a, int slice, int next = 0
 
 // ---- the largest logit of each slice; the rows' sums cleared
 __global__ void __launch_bounds__(256) sample_max_kernel(Args a) {
-    const int row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+    const int at = xcd_order(a.rows_n * a.slices), row = at / a.slices, slice = at % a.slices;
+    if (row >= a.rows_n) return;
     Row& r = a.rows[row];
     for (int i = slice * 256 + threadIdx.x; i < BINS; i += a.slices * 256) { r.mass[i] = 0; r.count[i] = 0; }
     if (slice == 0 && threadIdx.x == 0) r.list_n = 0;
@@ -237,7 +243,8 @@ template <int NT> __device__ __forceinline__ Plan plan(const u64* mass, const un
 __global__ void __launch_bounds__(256) sample_bins_kernel(Args a) {
     __shared__ u64 mass[BINS];
     __shared__ unsigned count[BINS];
-    const int row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+    const int at = xcd_order(a.rows_n * a.slices), row = at / a.slices, slice = at % a.slices;
+    if (row >= a.rows_n) return;
     const Params p = params(a, row);
     if (p.greedy) return;
     Row& r = a.rows[row];
@@ -267,9 +274,10 @@ __global__ void __launch_bounds__(256) sample_bins_kernel(Args a) {
 // ---- the tokens that the end of the row is decided on, and the weight of those that are certainly kept
 __global__ void __launch_bounds__(256) sample_gather_kernel(Args a) {
     __shared__ u64 s[4], list[LIST];       // with a plan of a list no slice has more
-    __shared__ unsigned listed, at;
+    __shared__ unsigned listed, base;
     __shared__ Plan shared;
-    const int row = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+    const int at = xcd_order(a.rows_n * a.slices), row = at / a.slices, slice = at % a.slices;
+    if (row >= a.rows_n) return;
     const Params p = params(a, row);
     if (!p.bins) return;
     Row& r = a.rows[row];
@@ -297,9 +305,9 @@ __global__ void __launch_bounds__(256) sample_gather_kernel(Args a) {
     __syncthreads();
     const unsigned n = min(listed, unsigned(LIST));
     if (n == 0) return;
-    if (threadIdx.x == 0) at = atomicAdd(&r.list_n, n);
+    if (threadIdx.x == 0) base = atomicAdd(&r.list_n, n);
     __syncthreads();
-    for (unsigned i = threadIdx.x; i < n && at + i < LIST; i += 256) r.list[at + i] = list[i];
+    for (unsigned i = threadIdx.x; i < n && base + i < LIST; i += 256) r.list[base + i] = list[i];
 }
 
 // ---- the row's token
@@ -605,7 +613,8 @@ __device__ __forceinline__ void end_greedy(const Args& a, int row, const Params&
 __global__ void __launch_bounds__(512) sample_pick_kernel(Args a) {
     constexpr int NT = 512;
     __shared__ Ends<NT> e;
-    const int row = blockIdx.x;
+    const int row = xcd_order(a.rows_n);
+    if (row >= a.rows_n) return;
     const Params p = params(a, row);
     if (p.greedy) return end_greedy(a, row, p);
     Row& r = a.rows[row];
@@ -709,16 +718,16 @@ hipError_t launch_sample(const SampleArgs& x, void* ws, size_t ws_bytes, hipStre
         int len = (x.vocab + slices - 1) / slices;
         slices = (x.vocab + len - 1) / len;
         if (held) { len = 64 * HELD; slices = (x.vocab + len - 1) / len; }
-        const Args a = {x.logits + size_t(r0) * x.row_stride, x.row_stride, x.vocab, slices, len, x.temperature ? x.temperature + r0 : nullptr,
+        const Args a = {x.logits + size_t(r0) * x.row_stride, x.row_stride, n, x.vocab, slices, len, x.temperature ? x.temperature + r0 : nullptr,
                         x.top_k ? x.top_k + r0 : nullptr, x.top_p ? x.top_p + r0 : nullptr, x.min_p ? x.min_p + r0 : nullptr, x.u + r0,
                         x.tokens + r0, x.logprobs ? x.logprobs + r0 : nullptr, (Row*)ws};
         if (held) {
             hipLaunchKernelGGL(sample_row_kernel, dim3(unsigned(n)), dim3(HELD_NT), 0, st, a);
         } else {
-            hipLaunchKernelGGL(sample_max_kernel, dim3(unsigned(n * slices)), dim3(256), 0, st, a);
-            hipLaunchKernelGGL(sample_bins_kernel, dim3(unsigned(n * slices)), dim3(256), 0, st, a);
-            if (x.top_k || x.top_p) hipLaunchKernelGGL(sample_gather_kernel, dim3(unsigned(n * slices)), dim3(256), 0, st, a);
-            hipLaunchKernelGGL(sample_pick_kernel, dim3(unsigned(n)), dim3(512), 0, st, a);
+            hipLaunchKernelGGL(sample_max_kernel, dim3(xcd_grid(n * slices)), dim3(256), 0, st, a);
+            hipLaunchKernelGGL(sample_bins_kernel, dim3(xcd_grid(n * slices)), dim3(256), 0, st, a);
+            if (x.top_k || x.top_p) hipLaunchKernelGGL(sample_gather_kernel, dim3(xcd_grid(n * slices)), dim3(256), 0, st, a);
+            hipLaunchKernelGGL(sample_pick_kernel, dim3(xcd_grid(n)), dim3(512), 0, st, a);
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
