@@ -457,7 +457,7 @@ attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restr
             const int key0 = ks.at(i) * 32;
             const bool more = i + 4 < c1, was_bad = bad;
             if (more) look_up(i + 4);
-            const bool edge = key0 + 31 > pos_lo || i1 - i0 + 1 < 16 * NB || (key0 <= pos_hi - window && key0 + 31 >= sinks);
+            const bool edge = key0 + 31 > pos_lo || (key0 <= pos_hi - window && key0 + 31 >= sinks);
             f32x4 sc[NB][2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
