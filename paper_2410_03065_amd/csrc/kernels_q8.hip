@@ -1041,7 +1041,7 @@ hipError_t merge_q8(const Q8View& v, int n_q, const KeyRanges& k, const AttnWs& 
 
 template <typename T, int HD, int NB, int NS>
 hipError_t attention_q8(const T* q, T* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws, hipStream_t st) {
-    const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 32, 2048, ws);
+    const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, 2048, ws);
     hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS>), dim3(unsigned(k.groups * k.splits)), dim3(256), 0, st, q, out, ws.part, v, n_q, window, sinks,
                        scale, k.chunk, k.splits, k.tiles);
     return merge_q8(v, n_q, k, ws, out, st);

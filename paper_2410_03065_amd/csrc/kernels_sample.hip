@@ -127,19 +127,29 @@ __device__ __forceinline__ double octaves(float l, const Params& r) {
     return l == r.top ? 0.0 : y;                    // also where both are infinite
 }
 __device__ __forceinline__ bool weighs(double y) { return y > -LEAST_OCTAVE; }
-// Its weight, 1 or more where it weighs.  2^f on |f| <= 1/2 by its Taylor polynomial in f ln 2: the first term left out is
-// 0.3466^12 / 12! = 6e-15.
+// Its weight where it weighs.  2^f on |f| <= 1/2 by the polynomial that meets it at the eleven Chebyshev points: 3e-16 off, 1 at
+// f = 0.  Adding a number with a unit of 1 in its last place rounds to a whole number and leaves it in the low bits.
 __device__ __forceinline__ u64 weight_at(double y) {
-    const double n = rint(y), f = (y - n) * 0.69314718055994530942;
-    double p = 1.0 / 39916800.0;
-    p = fma(p, f, 1.0 / 3628800.0); p = fma(p, f, 1.0 / 362880.0); p = fma(p, f, 1.0 / 40320.0); p = fma(p, f, 1.0 / 5040.0);
-    p = fma(p, f, 1.0 / 720.0); p = fma(p, f, 1.0 / 120.0); p = fma(p, f, 1.0 / 24.0); p = fma(p, f, 1.0 / 6.0);
-    p = fma(p, f, 0.5); p = fma(p, f, 1.0); p = fma(p, f, 1.0);
-    // adding 2^52 rounds to a whole number and leaves it in the low bits
-    const u64 w = u64(__double_as_longlong(ldexp(p, int(fmax(n, -64.0)) + 44) + 4503599627370496.0)) & 0xfffffffffffffull;
-    return weighs(y) ? max(u64(1), w) : 0;
+    const double whole = y + 6755399441055744.0;       // 1.5 * 2^52
+    const double f = y - (whole - 6755399441055744.0);
+    double p = 7.072585949269223e-09;
+    p = fma(p, f, 1.0208690299958306e-07); p = fma(p, f, 1.321544258792169e-06); p = fma(p, f, 1.5252657260200837e-05);
+    p = fma(p, f, 0.0001540353044173605); p = fma(p, f, 0.0013333558230164974); p = fma(p, f, 0.009618129107606888);
+    p = fma(p, f, 0.05550410866444772); p = fma(p, f, 0.24022650695910097); p = fma(p, f, 0.69314718055995); p = fma(p, f, 1.0);
+    const u64 scaled = u64(__double_as_longlong(p)) + (u64(unsigned(__double_as_longlong(whole)) + 44u) << 52);   // times 2^(n + 44)
+    return u64(__double_as_longlong(__longlong_as_double(scaled) + 4503599627370496.0)) & 0xfffffffffffffull;
 }
-__device__ __forceinline__ u64 weight(float l, const Params& r) { return weight_at(octaves(l, r)); }
+// 1 or more where it weighs
+__device__ __forceinline__ u64 weight(float l, const Params& r) {
+    const double y = octaves(l, r);
+    return weighs(y) ? max(u64(1), weight_at(y)) : 0;
+}
+// 0 below the least weight that is kept
+__device__ __forceinline__ u64 kept_weight(float l, const Params& r) {
+    const double y = octaves(l, r);
+    const u64 w = weight_at(y);
+    return weighs(y) && w >= r.least ? w : 0;
+}
 
 // The elements of a range, eight loads a thread at a time, of NT threads (64: each wave has a range of its own): f(element, its number).
 template <int NT, typename F> __device__ __forceinline__ void each(const float* l, int lo, int hi, F f) {
@@ -252,7 +262,7 @@ __global__ void __launch_bounds__(256) sample_bins_kernel(Args a) {
     const int lo = slice * a.slice_len, hi = min(a.vocab, lo + a.slice_len);
     if (!p.bins) {
         u64 sum = 0;
-        each<64>(l, part_begin(a, slice), part_begin(a, slice, 1), [&](float x, int) { const u64 w = weight(x, p); sum += w >= p.least ? w : 0; });
+        each<64>(l, part_begin(a, slice), part_begin(a, slice, 1), [&](float x, int) { sum += kept_weight(x, p); });
         sum = wave_sum(sum);
         if ((threadIdx.x & 63) == 0) r.part_mass[slice * 4 + (threadIdx.x >> 6)] = sum;
         return;
@@ -292,8 +302,7 @@ __global__ void __launch_bounds__(256) sample_gather_kernel(Args a) {
         const float t = place_of(x, p);
         if (!(t < end)) return;
         if (t < from) {
-            const u64 w = weight(x, p);
-            sum += w >= p.least ? w : 0;
+            sum += kept_weight(x, p);
         } else {
             const unsigned n = atomicAdd(&listed, 1u);
             if (n < LIST) list[n] = rank_key(x, i);
@@ -569,8 +578,7 @@ template <int NT> __device__ __forceinline__ void end_row(const Args& a, int row
         }
     }
     auto weight_of = [&](float x, int i) -> u64 {
-        const u64 w = weight(x, p);
-        return w >= p.least && rank_key(x, i) >= least_key ? w : 0;
+        return rank_key(x, i) >= least_key ? kept_weight(x, p) : 0;
     };
     // the parts' weights: known but for the list's tokens, or summed here
     const int parts = a.slices * 4, part_len = (a.slice_len + 3) / 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -586,9 +594,9 @@ template <int NT> __device__ __forceinline__ void end_row(const Args& a, int row
         }
     } else if (o.mode == BIN) {
         for (int i = threadIdx.x; i < listed; i += NT) {
-            const u64 k = e.list[i], w = weight_of_key(k);
+            const u64 k = e.list[i], w = kept_weight(unorder(unsigned(k >> 32)), p);
             const int id = int(~unsigned(k)), in = id % a.slice_len;
-            if (k >= least_key && w >= p.least) atomicAdd(&e.parts[id / a.slice_len * 4 + in / part_len], w);
+            if (k >= least_key && w) atomicAdd(&e.parts[id / a.slice_len * 4 + in / part_len], w);
         }
     }
     __syncthreads();
@@ -683,17 +691,29 @@ __global__ void __launch_bounds__(HELD_NT) sample_row_kernel(Args a) {
             o = plan<NT>(mass, count, p, e.s, &e.plan);
         }
     }
-    if (o.mode != DIGITS) {
-        const float from = o.mode == FRONT ? 0.f : float(o.last), end = float(o.last + 1);
+    if (o.mode == WHOLE) {
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+            u64 sum = 0;
+#pragma unroll
+            for (int k = part * 8; k < part * 8 + 8; ++k) sum += kept_weight(x[k], p);
+            sum = wave_sum(sum);
+            if (lane == 0) e.parts[wave * 4 + part] = sum;
+        }
+    } else if (o.mode == FRONT) {
+#pragma unroll
+        for (int k = 0; k < HELD; ++k)
+            if (place_of(x[k], p) < float(o.last + 1)) e.list[atomicAdd(&e.listed, 1u)] = rank_key(x[k], first + k * 64);
+    } else if (o.mode == BIN) {
+        const float from = float(o.last), end = float(o.last + 1);
 #pragma unroll
         for (int part = 0; part < 4; ++part) {
             u64 sum = 0;
 #pragma unroll
             for (int k = part * 8; k < part * 8 + 8; ++k) {
-                const float t = o.mode == WHOLE ? -1.f : place_of(x[k], p);
+                const float t = place_of(x[k], p);
                 if (t < from) {
-                    const u64 w = weight(x[k], p);
-                    sum += w >= p.least ? w : 0;
+                    sum += kept_weight(x[k], p);
                 } else if (t < end) {
                     e.list[atomicAdd(&e.listed, 1u)] = rank_key(x[k], first + k * 64);
                 }
