@@ -5,6 +5,7 @@
 // it lies in.  A score is therefore (q . c_j) * s_j and an output sum_j (p_j s'_j) c'_j: the products run on the codes as they
 // are, exact in bfloat16 (eight bits), and a scale is one factor per score.  No dequantised copy of the cache exists anywhere.
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <cmath>
 
@@ -1052,12 +1053,14 @@ hipError_t attention_q8_rows(const bf16_t* q, bf16_t* out, const Q8View& v, int 
                              hipStream_t st) {
     const KeyRanges k = key_ranges(v, n_q, 32 * NWV, 64, max_rows, max_len, window, sinks, 4, 1 << 20, 256, ws);
     constexpr int LDS = RowsLds<HD>::BYTES;
-    static bool set = false;
-    if (!set) {
-        const hipError_t e = hipFuncSetAttribute((const void*)attention_q8_rows_kernel<HD, NWV, NS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-        if (e != hipSuccess) return e;
-        set = true;
+    static std::atomic<uint64_t> set{0};                       // a bit per device
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e == hipSuccess && !(set.load(std::memory_order_relaxed) >> (device & 63) & 1)) {
+        e = hipFuncSetAttribute((const void*)attention_q8_rows_kernel<HD, NWV, NS>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+        if (e == hipSuccess) set.fetch_or(uint64_t(1) << (device & 63), std::memory_order_relaxed);
     }
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL((attention_q8_rows_kernel<HD, NWV, NS>), dim3(unsigned(k.groups * k.splits)), dim3(64 * NWV), LDS, st, q, out, ws.part, v, n_q, window,
                        sinks, scale, k.chunk, k.splits, k.tiles);
     return merge_q8(v, n_q, k, ws, out, st);
