@@ -178,3 +178,62 @@ def test_refusals():
     for i, v in ((0, None), (1, 99), (2, -1), (3, 0), (3, 2 ** 19 + 1), (8, None), (9, None)):
         assert call(*[v if j == i else a for j, a in enumerate(ok)]) == cake.E_INVAL, i
     assert call(*[0 if j == 2 else a for j, a in enumerate(ok)]) == cake.OK
+
+
+# Vocabularies on both sides of what one workgroup holds, and long ones, whose rows many workgroups share.
+@pytest.mark.parametrize("vocab", [2047, 32767, 32768, 32769, 40001])
+def test_around_the_longest_row_of_one_workgroup(vocab):
+    x, u, rng = rows_of(3, vocab)
+    check(x, u, 1.3)
+    check(x, u, 0.8, rng.integers(1, 300, 3), rng.uniform(0.5, 0.99, 3), rng.uniform(0.001, 0.1, 3))
+    check(x, u, top_k=[vocab // 2, 700, vocab - 1], top_p=[0.97, 0.5, 0.9])
+    for at in (0, vocab - 1):                     # the first and the last id
+        y = np.full((1, vocab), -np.inf, np.float32)
+        y[0, at] = -5.0
+        assert check(y, 0.7, top_k=3, top_p=0.5)[0] == at
+
+
+@pytest.mark.parametrize("vocab", [33000])
+def test_masks_ties_and_settings_of_long_rows(vocab):
+    low = np.finfo(np.float32).min
+    x, u, _ = rows_of(9, vocab)
+    x[0] = -np.inf
+    x[1] = np.nan
+    x[2, 100:] = -np.inf
+    x[3, 1:] = low
+    x[4] = low
+    x[5, :30000] = np.nan
+    x[6, 17] = np.inf
+    x[7, [5, 31000]] = np.inf
+    x[8] = 0.0
+    x[8, 7:] = -0.0
+    for more in ({}, dict(top_k=20), dict(top_k=9000, top_p=0.6), dict(top_p=0.7), dict(min_p=0.01), dict(top_k=30, top_p=0.8, min_p=0.02),
+                 dict(temperature=0.0), dict(temperature=1e-30), dict(temperature=1e30, top_p=0.9)):
+        check(x, u, **more)
+
+
+@pytest.mark.parametrize("vocab", [3000, 40000])
+def test_logits_and_temperatures_at_the_ends_of_the_range(vocab):
+    """Logits whose difference passes float32's largest number, and differences that only a tiny temperature tells apart."""
+    x, u, rng = rows_of(3, vocab)
+    for settings in (dict(), dict(top_k=40), dict(top_p=0.9), dict(top_k=100, top_p=0.8, min_p=0.01)):
+        check(x * np.float32(1.7e37), u, temperature=2e37, **settings)
+        check(x * np.float32(1e-38), u, temperature=1e-38, **settings)
+        check(x * np.float32(1e-40), u, temperature=1e-40, **settings)
+
+
+def test_graph_replays_of_long_rows():
+    import torch
+    x, u, _ = rows_of(4, 40000)
+    d, du = torch.from_numpy(x).cuda(), torch.from_numpy(u).cuda()
+    k, p = torch.tensor([0, 40, 0, 5000], dtype=torch.int32).cuda(), torch.tensor([1.0, 0.9, 0.95, 0.9]).cuda()
+    graph = torch.cuda.CUDAGraph()
+    eng().op_sample(d, du, top_k=k, top_p=p)
+    with torch.cuda.graph(graph):
+        got = eng().op_sample(d, du, top_k=k, top_p=p)
+    for seed in range(4):
+        x, u, _ = rows_of(4, 40000, seed)
+        d.copy_(torch.from_numpy(x)), du.copy_(torch.from_numpy(u))
+        graph.replay()
+        again = got[0].clone()
+        np.testing.assert_array_equal(again.cpu().numpy(), check(x, u, top_k=k.cpu().numpy(), top_p=p.cpu().numpy()))
