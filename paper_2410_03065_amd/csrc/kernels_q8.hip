@@ -1010,7 +1010,11 @@ hipError_t append_q8(const float* qkv, T* q, T* values, const Q8View& v, const c
     return go(std::integral_constant<int, ROPE_HALVES_PART>{});
 }
 
-// How a launch divides the keys: `chunk` steps of `width` keys to a workgroup, at most `splits` ranges.
+// How a launch divides the keys: `chunk` steps of `width` keys to a workgroup, at most `splits` ranges.  About `want` workgroups
+// of `least` steps or more.  Tiles of 16 and 32 rows: 2048 of 4 to 48 steps (64 ragged sequences up to 8191 keys, with the merge:
+// 4 steps 158 us, 12 144, 24 133, 32 138, 48 133, 64 149, 129 155; one of 701: 4 steps 10.1, 8 11.2, 24 13.1 without a merge).
+// Tiles of 128 rows: 512, two a compute unit (16 ragged sequences, 128 rows: 256 116 us, 512 81, 1024 87); of 256: 256 (one of
+// 16000 keys: 256 48 us, 512 65).
 struct KeyRanges { int tiles, chunk, splits; int64_t groups; };
 KeyRanges key_ranges(const Q8View& v, int n_q, int rows_per_tile, int width, int max_rows, int max_len, int window, int sinks, int least, int most, int64_t want,
                      const AttnWs& ws) {
@@ -1051,7 +1055,7 @@ hipError_t attention_q8(const T* q, T* out, const Q8View& v, int n_q, int max_ro
 template <int HD, int NWV, int NS>
 hipError_t attention_q8_rows(const bf16_t* q, bf16_t* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws,
                              hipStream_t st) {
-    const KeyRanges k = key_ranges(v, n_q, 32 * NWV, 64, max_rows, max_len, window, sinks, 4, 1 << 20, 256, ws);
+    const KeyRanges k = key_ranges(v, n_q, 32 * NWV, 64, max_rows, max_len, window, sinks, 4, 1 << 20, NWV == 8 ? 256 : 512, ws);
     constexpr int LDS = RowsLds<HD>::BYTES;
     static std::atomic<uint64_t> set{0};                       // a bit per device
     int device = 0;
@@ -1085,10 +1089,22 @@ hipError_t launch_attention_q8(int dtype, const void* q, void* out, const Q8View
         if (dtype == CAKE_F32) return attention_q8<float, HD, 1, NS>((const float*)q, (float*)out, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
         const bf16_t* qb = (const bf16_t*)q;
         bf16_t* ob = (bf16_t*)out;
-        if (rows <= 16) return attention_q8<bf16_t, HD, 1, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
-        if (rows <= 32) return attention_q8<bf16_t, HD, 2, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
-        if (rows <= 128) return attention_q8_rows<HD, 4, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
-        return attention_q8_rows<HD, 8, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
+        // Tiles of 32 rows where one holds them all: 33 sequences up to 4099, 20 rows, heads of 64: 45 us, 50 with two tiles of 16.
+        if (rows > 16 && rows <= 32) return attention_q8<bf16_t, HD, 2, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
+        // Heads of 128: what a tile costs, in halves of a tile of 16 rows.  Measured (us; tiles of 16, of 128, of 256 rows), 32 / 8 heads:
+        // 16 sequences of 8191 keys: 36 rows 82, 144, -; 96 rows 159, 145, 251; 192 rows 253, 264, 251; 256 rows 326, 266, 251;
+        // 16 ragged ones up to 4099: 36 rows 40, 78, -; 128 rows 73, 81, 116; 132 rows 73, 133, 128; 256 rows 101, 140, 128;
+        // 1 of 16000: 36 rows 46, 42, -; 128 rows 53, 44, -; 256 rows 79, 52, 48; 4 of 4096, 512 rows: 97, 82, 75.
+        if constexpr (HD == 128) {
+            const int64_t few = 2 * ((rows + 15) / 16), four = 13 * ((rows + 127) / 128), eight = 24 * ((rows + 255) / 256);
+            if (four < few && four < eight) return attention_q8_rows<HD, 4, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
+            if (eight <= few) return attention_q8_rows<HD, 8, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
+        // Heads of 64, half the bytes and products at the same other work: 1 of 16000: 192 rows 42, 45, 48; 512 rows 85, 66, 73;
+        // 1024 rows 159, 109, 123; 4 of 4096: 512 rows 61, 74, 83; 1024 rows 111, 133, 133; 16 of 8191: 256 rows 194, 242, 327.
+        } else if (rows >= 512) {
+            return attention_q8_rows<HD, 4, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
+        }
+        return attention_q8<bf16_t, HD, 1, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
     };
     const std::integral_constant<int, 128> hd128{};
     const std::integral_constant<int, 64> hd64{};
