@@ -558,7 +558,8 @@ typedef struct {
     int32_t n_physical_pages;   /* pages per layer in the pool */
     int32_t n_rows;             /* rows of the batch's activations */
     int32_t max_rows;           /* most rows of one sequence and ... */
-    int32_t max_len;            /* ... most tokens of one: they choose kernels and launch sizes, results do not depend on them (0: unknown) */
+    int32_t max_len;            /* ... most tokens of one: they choose kernels and launch sizes, results depend on them
+                                 * no further than the roundings that cake_op_attention_q8 states (0: unknown) */
 } cake_q8_batch;
 
 /* Bytes of one layer page, 0 if the sizes are not supported.  Pure. */
@@ -607,8 +608,8 @@ int32_t cake_op_append_q8(cake_ctx* ctx, const float* qkv, void* q, void* values
 /* out[n_rows][n_q * head_dim] = attention of q[n_q][n_rows][head_dim] (both device, model dtype) over layer `layer`: the row at
  * position p sees keys j <= p, with window > 0 only those with p - j < window or j < sinks.  A row that sees no key is zeros.  Scores,
  * softmax and sums in float32; on the way into the second product bf16 models round a weight times its
- * value's scale to 16 bits, or, with more than 32 rows (n_q / n_kv of them a token), to 11 bits, and to 2^-28 of the row's largest weight times
- * the largest scale of the key's 64 tokens.
+ * value's scale to 16 bits, or, with many rows (n_q / n_kv of them a token; heads of 128: more than 96, heads of 64: 512 or more), to 11 bits,
+ * and to 2^-28 of the row's largest weight times the largest scale of the key's 64 tokens.
  * Pointers 16-byte aligned.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
                              const cake_q8_batch* batch);
@@ -624,7 +625,7 @@ int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t la
  * A logit of -infinity or NaN is never chosen; with +infinity only those are.  A row with nothing to choose gives token -1 and
  * log-probability -infinity.  tokens: int32; logprobs: float32, log of the token's probability among those that stayed, or NULL.
  * Probabilities below 2^-45 of the likeliest one's count as 0.  The result does not depend on the batch that a row is in.
- * vocab <= 2^19, row_stride >= vocab.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
+ * rows <= 2^20, vocab <= 2^19, row_stride >= vocab.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_sample(cake_ctx* ctx, const float* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
                        const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tokens, float* logprobs);
 

@@ -127,6 +127,7 @@ class Q8Batch(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("pool", "block_table", "seq_len", "row_begin")] + \
                [(n, C.c_int32) for n in ("n_seqs", "pages_per_seq", "page_tokens", "scale_tokens", "n_physical_pages", "n_rows", "max_rows",
                                          "max_len")]
+    model = None     # (layers, KV heads, head size) of the pages, where an Engine has described them
 
 
 ROPE_LAYOUTS = {"pairs": 0, "halves": 1}
@@ -341,7 +342,8 @@ class Engine:
     stream was given before them (their operands come from there); the others do not: synchronise
     after torch has written to the pool.  op_append_q8, op_attention_q8 and op_sample return before their work is done: it runs
     in order with torch's current stream, without a wait where that is the compute stream.
-    compute_stream: a torch stream of the default priority to use as the compute stream (None: one of the engine's own)."""
+    compute_stream: a torch stream of the default priority to use as the compute stream (None: one of the engine's own).
+    An engine on torch's default stream runs such calls with the least delay, but they cannot be captured into a graph."""
 
     def __init__(self, shape, weights=None, *, max_tokens, max_chunk, page_tokens=256, block_table=None,
                  n_physical_pages=None, device="cuda:0", seed=0, with_head=False, compute_stream=None):
@@ -351,6 +353,7 @@ class Engine:
         if not torch.cuda.is_available():
             raise CakeError(E_STATE, "no GPU: the HIP path cannot run and there is no CPU fallback")
         self.shape = shape
+        self._q8_model = (shape.n_layers, shape.n_kv, shape.head_dim)
         self.dev = torch.device(device)
         torch.cuda.set_device(self.dev)
         self.tdtype = torch.float32 if shape.dtype == "f32" else torch.bfloat16
@@ -815,11 +818,19 @@ class Engine:
             rc = fn(self.ctx, *args)
         else:
             current = self.torch.cuda.current_stream(self.dev)
+            if self._compute_raw == 0 and self.torch.cuda.is_current_stream_capturing():
+                raise CakeError(E_STATE, "%s: an engine on the default stream cannot be captured: no graph holds that stream's work" % what)
             self.compute_stream.wait_stream(current)
             rc = fn(self.ctx, *args)
             current.wait_stream(self.compute_stream)
         if rc != OK:
             self._check(rc, what)
+
+    def _batch(self, batch):
+        """The batch, or a refusal where it describes pages of another model."""
+        if batch.model is not self._q8_model and batch.model not in (None, self._q8_model):
+            raise CakeError(E_INVAL, "batch: described for (layers, KV heads, head size) %s, not %s" % (batch.model, self._q8_model))
+        return batch
 
     def _operand(self, t, name, dtype, shape=None):
         """Address of a contiguous tensor on the engine's device, or a refusal."""
@@ -847,13 +858,13 @@ class Engine:
         b = Q8Batch(self._operand(pool, "pool", torch.uint8), self._operand(block_table, "block_table", torch.int32),
                     self._operand(seq_len, "seq_len", torch.int32, (n,)), self._operand(row_begin, "row_begin", torch.int32, (n + 1,)),
                     n, block_table.shape[1], page_tokens, scale_tokens, pool.numel() // (page * self.shape.n_layers), n_rows, max_rows, max_len)
-        b.tensors = (pool, block_table, seq_len, row_begin)
+        b.tensors, b.model = (pool, block_table, seq_len, row_begin), self._q8_model
         return b
 
     def op_append_q8(self, qkv, layer, batch, rope, q=None, want_values=False):
         """qkv float32 [n_rows][(n_q + 2 n_kv) hd] -> q [n_q][n_rows][hd], rotated; keys and values into the pages.  want_values:
         (q, values [n_rows][2 n_kv][hd] as the pages now hold them)."""
-        s, n = self.shape, batch.n_rows
+        s, n = self.shape, self._batch(batch).n_rows
         if q is None:
             q = self.torch.empty((s.n_q, n, s.head_dim), dtype=self.tdtype, device=self.dev)
         values = self.torch.empty((n, 2 * s.n_kv, s.head_dim), dtype=self.tdtype, device=self.dev) if want_values else None
@@ -864,7 +875,7 @@ class Engine:
 
     def op_attention_q8(self, q, layer, batch, window=0, sinks=0, out=None):
         """q [n_q][n_rows][hd] -> [n_rows][n_q * hd] (cake_op_attention_q8)."""
-        s, n = self.shape, batch.n_rows
+        s, n = self.shape, self._batch(batch).n_rows
         if out is None:
             out = self.torch.empty((n, s.n_q * s.head_dim), dtype=self.tdtype, device=self.dev)
         self._in_order(self.lib.cake_op_attention_q8, "cake_op_attention_q8", self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)),

@@ -6,7 +6,7 @@ import pytest
 
 import synth_inputs as si
 from oracle import serving
-from q8_helpers import attention_bound
+from q8_helpers import Batch, attention_bound, engine
 
 pytestmark = pytest.mark.gpu
 PT = 64
@@ -106,3 +106,33 @@ def test_steps_replayed_from_a_graph():
         want = step(other, other_lens)
         torch.cuda.synchronize()
         assert torch.equal(tokens, want) and torch.equal(pool, other) and torch.equal(lens, other_lens)
+
+
+def test_a_batch_of_another_model_is_refused():
+    import torch
+    import paper_2410_03065_amd as cake
+    b = Batch(engine(4, 2, 64, "bf16"), [70], [1])
+    other, same = engine(4, 4, 64, "bf16"), engine(8, 2, 64, "bf16")
+    with pytest.raises(cake.CakeError):
+        other.op_attention_q8(torch.zeros((4, 1, 64), dtype=torch.bfloat16, device="cuda"), 0, b.q8)
+    with pytest.raises(cake.CakeError):
+        other.op_append_q8(torch.zeros((1, 12 * 64), device="cuda"), 0, b.q8, cake.rope(10000.0, 64))
+    assert same.op_attention_q8(torch.zeros((8, 1, 64), dtype=torch.bfloat16, device="cuda"), 0, b.q8).shape == (1, 512)
+
+
+def test_an_engine_on_the_default_stream_refuses_a_capture():
+    import torch
+    import paper_2410_03065_amd as cake
+    eng = engine(4, 2, 64, "bf16", compute_stream=torch.cuda.default_stream())
+    b = Batch(eng, [70], [1])
+    q = torch.zeros((4, 1, 64), dtype=torch.bfloat16, device="cuda")
+    want = eng.op_attention_q8(q, 0, b.q8).clone()
+    held = torch.zeros(4, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held.add_(1)
+        with pytest.raises(cake.CakeError) as e:
+            eng.op_attention_q8(q, 0, b.q8)
+    assert e.value.code == cake.E_STATE
+    graph.replay()
+    assert held.tolist() == [1.0] * 4 and torch.equal(eng.op_attention_q8(q, 0, b.q8), want)
