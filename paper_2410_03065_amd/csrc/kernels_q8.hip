@@ -103,13 +103,14 @@ enum RopeMode { ROPE_ADJACENT, ROPE_HALVES, ROPE_HALVES_PART };
 // Two kinds of workgroups.  Rows: eight tokens of a sequence and some of the heads, sixteen heads' rows at a time, four more on
 // their way; with a scale per token that is all.  Blocks, where tokens share scales: 64 positions (whole blocks, aligned, so no
 // two workgroups write one) of one KV head, whose keys and values stay in registers between the largest magnitude and the codes.
-// Bound by the bytes: 4 read per element, 1 or 2 written; 2447 tokens of 64 / 8 heads of 128, a scale for 64: 48 us, 3.2 TB/s.  The rotation runs in 64 bits, full rate on this chip: at position 60000
+// They take longest and come first in the grid (last: 49 us, first: 38).
+// Bound by the bytes: 4 read per element, 1 or 2 written; 2447 tokens of 64 / 8 heads of 128, a scale for 64: 38 us, 4.1 TB/s.  The rotation runs in 64 bits, full rate on this chip: at position 60000
 // a float32 angle is off by 4e-3, and the codes that follow are whole numbers, which with the rotated value correctly rounded to
 // float32 hardly depend on how cosine and sine were come by.
 template <typename T, int HD, int MODE>
 __global__ void __launch_bounds__(256)
 append_q8_kernel(const float* __restrict__ qkv, T* __restrict__ q, T* __restrict__ values, Q8View v, cake_rope rope, int n_q, int row_tiles, int chunks,
-                 int row_groups, int block_tiles) {
+                 int block_groups, int block_tiles) {
     constexpr int E = HD / 16, P = MODE == ROPE_HALVES ? E / 2 : E, S = MODE == ROPE_HALVES ? HD / 2 : 0;   // elements a lane, in a piece; pieces apart
     constexpr int TOKENS = 8, AT_ONCE = 4, HELD = 8;
     typedef typename Vec<float, P < 4 ? P : 4>::type Piece;
@@ -219,9 +220,9 @@ append_q8_kernel(const float* __restrict__ qkv, T* __restrict__ q, T* __restrict
         return double2{z.x * rope.magnitude, z.y * rope.magnitude};
     };
 
-    if (int(blockIdx.x) < row_groups) {
+    if (int(blockIdx.x) >= block_groups) {
         // ---- rows
-        int b = blockIdx.x;
+        int b = int(blockIdx.x) - block_groups;
         const int chunk = b % chunks; b /= chunks;
         const int t0 = b % row_tiles, s = b / row_tiles;
         const Seq seq = sequence(v, s);
@@ -259,7 +260,7 @@ append_q8_kernel(const float* __restrict__ qkv, T* __restrict__ q, T* __restrict
         return;
     }
     // ---- blocks
-    int b = blockIdx.x - row_groups;
+    int b = blockIdx.x;
     const int g = b % v.n_kv; b /= v.n_kv;
     const int t0 = b % block_tiles, s = b / block_tiles;
     const Seq seq = sequence(v, s);
@@ -1007,7 +1008,7 @@ hipError_t append_q8(const float* qkv, T* q, T* values, const Q8View& v, const c
     const int row_groups = v.n_seqs * row_tiles * chunks, block_groups = v.n_seqs * block_tiles * v.n_kv;
     auto go = [&](auto mode) {
         hipLaunchKernelGGL((append_q8_kernel<T, HD, decltype(mode)::value>), dim3(unsigned(row_groups + block_groups)), dim3(256), 0, st, qkv, q, values, v, rope,
-                           n_q, row_tiles, chunks, row_groups, block_tiles);
+                           n_q, row_tiles, chunks, block_groups, block_tiles);
         return hipGetLastError();
     };
     if (rope.layout == CAKE_ROPE_PAIRS) return go(std::integral_constant<int, ROPE_ADJACENT>{});
