@@ -359,8 +359,8 @@ template <int W> __device__ __forceinline__ KeySteps<W> key_steps(int pos_lo, in
 template <typename T> struct Terms { static constexpr int Q = 1, W = 2; };
 template <> struct Terms<float> { static constexpr int Q = 3, W = 3; };
 
-template <typename T, int HD, int NB, int NS>
-__global__ void __launch_bounds__(256, NB == 2 || Terms<T>::Q == 3 ? 2 : HD == 128 ? 3 : 4)
+template <typename T, int HD, int NB, int NS, int NW>
+__global__ void __launch_bounds__(64 * NW, NW == 8 || NB == 2 || Terms<T>::Q == 3 ? 2 : HD == 128 ? 3 : 4)
 attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict__ part, Q8View v, int n_q, int window, int sinks,
                     float scale_log2, int chunk, int splits, int tiles) {
     constexpr int TQ = Terms<T>::Q, TW = Terms<T>::W;
@@ -456,10 +456,10 @@ attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restr
         };
         int i = c0 + wave;
         if (i < c1) { look_up(i); load_keys(); load_values(); }
-        for (; i < c1; i += 4) {
+        for (; i < c1; i += NW) {
             const int key0 = ks.at(i) * 32;
-            const bool more = i + 4 < c1, was_bad = bad;
-            if (more) look_up(i + 4);
+            const bool more = i + NW < c1, was_bad = bad;
+            if (more) look_up(i + NW);
             const bool edge = key0 + 31 > pos_lo || (key0 <= pos_hi - window && key0 + 31 >= sinks);
             f32x4 sc[NB][2];
 #pragma unroll
@@ -530,20 +530,38 @@ attention_q8_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restr
             }
             if (more) load_values();
         }
-        // the four waves' parts, added up in their order
+        // the waves' parts, added up in their order: of eight the upper four's first, each to the wave four below
 #pragma unroll
         for (int r = 0; r < NB; ++r) {
             if (r) __syncthreads();
-            const float lt = sum4(l[r]);
-            if (g4 == 0) { s_ml[wave][n16][0] = m[r]; s_ml[wave][n16][1] = lt; }
+            float lt = sum4(l[r]);
+            auto leave = [&](int w) {
+                if (g4 == 0) { s_ml[w][n16][0] = m[r]; s_ml[w][n16][1] = lt; }
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int j = 0; j < CW; j += 4)
-                    *(float4*)&s_acc[wave][n16][(4 * g4 + e) * CW + j] = make_float4(acc[r][j][e], acc[r][j + 1][e], acc[r][j + 2][e], acc[r][j + 3][e]);
+                    for (int j = 0; j < CW; j += 4)
+                        *(float4*)&s_acc[w][n16][(4 * g4 + e) * CW + j] = make_float4(acc[r][j][e], acc[r][j + 1][e], acc[r][j + 2][e], acc[r][j + 3][e]);
+            };
+            if constexpr (NW == 8) {
+                if (wave >= 4) leave(wave - 4);
+                __syncthreads();
+                if (wave < 4) {
+                    const float other = s_ml[wave][n16][0], top = fmaxf(m[r], other);
+                    const float f = __builtin_amdgcn_exp2f(m[r] - top), h = __builtin_amdgcn_exp2f(other - top);
+                    lt = lt * f + s_ml[wave][n16][1] * h;
+                    m[r] = top;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int j = 0; j < CW; ++j) acc[r][j][e] = acc[r][j][e] * f + s_acc[wave][n16][(4 * g4 + e) * CW + j] * h;
+                }
+                __syncthreads();
+            }
+            if (wave < 4) leave(wave);
             __syncthreads();
             const int row = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * CW, idx = i0 + 16 * r + row;
-            if (idx < n) {
+            if (row < 16 && idx < n) {
                 float mt = s_ml[0][row][0];
 #pragma unroll
                 for (int w = 1; w < 4; ++w) mt = fmaxf(mt, s_ml[w][row][0]);
@@ -1021,14 +1039,14 @@ hipError_t append_q8(const float* qkv, T* q, T* values, const Q8View& v, const c
 // 4 steps 158 us, 12 144, 24 133, 32 138, 48 133, 64 149, 129 155; one of 701: 4 steps 10.1, 8 11.2, 24 13.1 without a merge).
 // Tiles of 128 rows: 512, two a compute unit (16 ragged sequences, 128 rows: 256 116 us, 512 81, 1024 87); of 256: 256 (one of
 // 16000 keys: 256 48 us, 512 65).
-struct KeyRanges { int tiles, chunk, splits; int64_t groups; };
+struct KeyRanges { int tiles, chunk, splits; int64_t steps, groups; };
 KeyRanges key_ranges(const Q8View& v, int n_q, int rows_per_tile, int width, int max_rows, int max_len, int window, int sinks, int least, int most, int64_t want,
                      const AttnWs& ws) {
     KeyRanges k;
     const int G = n_q / v.n_kv;
     k.tiles = int(std::min<int64_t>((int64_t(max_rows) * G + rows_per_tile - 1) / rows_per_tile, std::max(1, MOST_GROUPS / (v.n_seqs * v.n_kv))));
     const int64_t seen = std::min<int64_t>(max_len, int64_t(window) + sinks + rows_per_tile / G + 2 * width);
-    const int64_t steps = seen / width + 1;
+    const int64_t steps = k.steps = seen / width + 1;
     k.groups = int64_t(v.n_seqs) * v.n_kv * k.tiles;
     int64_t chunk = std::min<int64_t>(std::max<int64_t>(least, (steps * k.groups + want - 1) / want), most);
     chunk = std::max(chunk, steps * k.groups / 16384);        // ranges past a sequence's end cost a little too
@@ -1052,8 +1070,18 @@ hipError_t merge_q8(const Q8View& v, int n_q, const KeyRanges& k, const AttnWs& 
 
 template <typename T, int HD, int NB, int NS>
 hipError_t attention_q8(const T* q, T* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws, hipStream_t st) {
-    const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, 2048, ws);
-    hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS>), dim3(unsigned(k.groups * k.splits)), dim3(256), 0, st, q, out, ws.part, v, n_q, window, sinks,
+    KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, 2048, ws);
+    // Short sequences on eight waves, undivided: no merge.  Measured (us, against four waves with the merge, 8 KV heads of 128, a token each):
+    // 1 sequence of 300 keys 7.5, 9.0; 701: 11.1, 9.6; 1500: 16.4, 10.0; 8 of 300: 7.7, 9.5; 701: 11.8, 11.8; 1500: 18.9, 14.4;
+    // 32 of 300: 9.4, 13.8; 701: 13.4, 19.2; 1500: 23.2, 32.3; 64 of 1500: 44.7, 50.8; 256 of 300: 60.0, 40.8.
+    if constexpr (NB == 1) {
+        if (k.groups <= 512 && k.steps <= 12 + k.groups / 6) {
+            hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS, 8>), dim3(unsigned(k.groups)), dim3(512), 0, st, q, out, ws.part, v, n_q, window, sinks,
+                               scale, int(k.steps), 1, k.tiles);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS, 4>), dim3(unsigned(k.groups * k.splits)), dim3(256), 0, st, q, out, ws.part, v, n_q, window, sinks,
                        scale, k.chunk, k.splits, k.tiles);
     return merge_q8(v, n_q, k, ws, out, st);
 }

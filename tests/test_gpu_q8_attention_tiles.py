@@ -102,3 +102,19 @@ def test_graph_replays_with_other_contents(hd, rows):
         graph.replay()
         got = out.clone()
         assert torch.equal(got, b.eng.op_attention_q8(q, 0, b.q8))
+
+
+@pytest.mark.parametrize("kind,n_kv,hd,seqs", [("bf16", 8, 64, 64), ("bf16", 8, 64, 65), ("bf16", 2, 128, 300), ("f32", 4, 64, 140)])
+def test_many_short_sequences(kind, n_kv, hd, seqs):
+    """Short sequences undivided on eight waves, or, where there are many, on four."""
+    lens = np.random.default_rng(seqs).integers(1, 260, seqs)
+    lens[:3] = 0, 256, 257
+    b = Batch(engine(2 * n_kv, n_kv, hd, kind), lens, [1] * seqs, pt=64, seed=seqs)
+    check(b)
+    check(b, window=40, sinks=3)
+
+
+@pytest.mark.parametrize("keys", [250, 600, 700, 1400])
+def test_few_sequences_on_both_sides_of_the_division(keys):
+    for seqs in (1, 4, 16):
+        check(Batch(engine(8, 2, 128, "bf16"), [keys] * (seqs - 1) + [keys - 7], [1] * seqs, pt=64, seed=keys))
