@@ -348,7 +348,7 @@ template <int W> __device__ __forceinline__ KeySteps<W> key_steps(int pos_lo, in
 }
 
 // Few rows.  A tile is NB x 16 rows (token, query head of the group) of one sequence and KV head; a workgroup takes a range of
-// its key steps, its four waves every fourth step each, straight from memory into registers.  Scores are formed transposed,
+// its key steps, its four (eight) waves every fourth (eighth) step each, straight from memory into registers.  Scores are formed transposed,
 // S^T[key][row] = K Q^T, so that a lane holds four keys of one row per block of 16 and the weights are the second product's
 // operand as they are: O^T[hd][row] += V^T W^T, where the slots of a product are dealt to keys as the scores lie (slot
 // 8g + t: key 4g + t, from t = 4 key 16 + 4g + t - 4).  A lane reads 8 (4) neighbouring elements of eight keys' values and
@@ -1070,16 +1070,17 @@ hipError_t merge_q8(const Q8View& v, int n_q, const KeyRanges& k, const AttnWs& 
 
 template <typename T, int HD, int NB, int NS>
 hipError_t attention_q8(const T* q, T* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws, hipStream_t st) {
-    KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, 2048, ws);
-    // Short sequences on eight waves, undivided: no merge.  Measured (us, against four waves with the merge, 8 KV heads of 128, a token each):
-    // 1 sequence of 300 keys 7.5, 9.0; 701: 11.1, 9.6; 1500: 16.4, 10.0; 8 of 300: 7.7, 9.5; 701: 11.8, 11.8; 1500: 18.9, 14.4;
-    // 32 of 300: 9.4, 13.8; 701: 13.4, 19.2; 1500: 23.2, 32.3; 64 of 1500: 44.7, 50.8; 256 of 300: 60.0, 40.8.
-    if constexpr (NB == 1) {
-        if (k.groups <= 512 && k.steps <= 12 + k.groups / 6) {
-            hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS, 8>), dim3(unsigned(k.groups)), dim3(512), 0, st, q, out, ws.part, v, n_q, window, sinks,
-                               scale, int(k.steps), 1, k.tiles);
-            return hipGetLastError();
-        }
+    const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, 2048, ws);
+    // Undivided on eight waves, without a merge, where that fills the compute units once and sequences are not too long for it.  Measured
+    // (us, against four waves, divided, with the merge; 8 KV heads of 128, a token each; sequences x keys): 1 x 300 7.5, 9.0;
+    // 1 x 701 11.1, 9.6; 8 x 300 7.7, 9.5; 8 x 1500 18.9, 14.4; 16 x 1000 15.0, 17.4; 24 x 1500 20.0, 27.1; 32 x 701 13.4, 19.2;
+    // 32 x 4100 53.8, 65.6; 48 x 4100 94.0, 86.6; 64 x 1500 44.7, 50.8; 64 ragged up to 8191 147.7, 132.8; 256 x 300 60.0, 40.8; 33 ragged
+    // ones up to 4099, 20 rows, heads of 64 39.1, 42.4.
+    const int64_t most_steps = k.groups <= 288 ? std::min<int64_t>(130, 12 + k.groups * k.groups / 550) : k.groups <= 512 ? 50 : 0;
+    if (k.steps <= most_steps) {
+        hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS, 8>), dim3(unsigned(k.groups)), dim3(512), 0, st, q, out, ws.part, v, n_q, window, sinks, scale,
+                           int(k.steps), 1, k.tiles);
+        return hipGetLastError();
     }
     hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS, 4>), dim3(unsigned(k.groups * k.splits)), dim3(256), 0, st, q, out, ws.part, v, n_q, window, sinks,
                        scale, k.chunk, k.splits, k.tiles);
