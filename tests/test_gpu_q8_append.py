@@ -198,3 +198,8 @@ def test_refusals():
         bad = cake.Rope.from_buffer_copy(rope)
         setattr(bad, field, value)
         assert call(x.data_ptr(), q.data_ptr(), None, 0, ctypes.byref(bad), d) == cake.E_INVAL
+
+
+@pytest.mark.parametrize("block", [1, 16, 64])
+def test_pages_of_192_tokens(block):
+    check(Batch(engine(8, 4, 64, "bf16"), [500, 193, 192, 64], [300, 1, 2, 64], pt=192, block=block))

@@ -118,3 +118,10 @@ def test_many_short_sequences(kind, n_kv, hd, seqs):
 def test_few_sequences_on_both_sides_of_the_division(keys):
     for seqs in (1, 4, 16):
         check(Batch(engine(8, 2, 128, "bf16"), [keys] * (seqs - 1) + [keys - 7], [1] * seqs, pt=64, seed=keys))
+
+
+@pytest.mark.parametrize("rows", [1, 30, 70])
+def test_pages_of_an_odd_number_of_steps(rows):
+    b = Batch(engine(8, 2, 128, "bf16"), [500, 193, 192, 70 + rows], [rows, rows, 1, rows], pt=192, block=16)
+    check(b)
+    check(b, window=100, sinks=5)
