@@ -847,7 +847,8 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const float t = max4(top[r]);
-                    const float by = t > W_TOP || (sum4(l[r]) == 0.f && t > -INFINITY) ? t - W_FIRST : 0.f, f = FIRST ? 0.f : __builtin_amdgcn_exp2f(-by);
+                    const bool none = FIRST || sum4(l[r]) == 0.f;      // nothing summed yet, so nothing to rescale: the factor of a low t would be infinite
+                    const float by = t > W_TOP || (none && t > -INFINITY) ? t - W_FIRST : 0.f, f = none ? 0.f : __builtin_amdgcn_exp2f(-by);
                     m[r] += by;
                     if constexpr (!FIRST) {
                         l[r] *= f;
