@@ -633,6 +633,7 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                          float scale_log2, int chunk, int splits, int tiles) {
     constexpr int ROWS = 32 * NWV, HALF = 32 * NWV, CPT = 64 * HD / HALF, VC = CPT / 8;   // threads that stage one half; codes and columns of each
     constexpr int QC = HD / 32, HB = HD / 16;
+    static_assert(VC == 4 || VC == 8, "values are loaded in pieces of four or eight codes");
     typedef RowsLds<HD> L;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g4 = lane >> 4;
@@ -706,8 +707,7 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
                 for (int t = 0; t < 8; ++t) {
                     const unsigned char* p = codes + v_from + (t < 4 ? t : t + 12) * HD;
                     if constexpr (VC == 8) *(uint2*)&raw[2 * t] = *(const uint2*)p;
-                    else if constexpr (VC == 4) raw[t] = *(const unsigned*)p;
-                    else raw[t / 2] = t & 1 ? raw[t / 2] | unsigned(*(const unsigned short*)p) << 16 : *(const unsigned short*)p;
+                    else raw[t] = *(const unsigned*)p;
                 }
             }
         };
@@ -716,10 +716,7 @@ attention_q8_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out,
             if constexpr (decltype(keys_)::value) {
                 *(bf16x8*)(base + (k_put ^ (c << 4))) = codes8(raw[2 * c], raw[2 * c + 1]);
             } else {
-                auto val = [&](int t) {
-                    const unsigned w = VC == 8 ? raw[2 * t + c / 4] : VC == 4 ? raw[t] : raw[t / 2];
-                    return code(w, VC == 2 ? 2 * (t & 1) + c : c & 3);
-                };
+                auto val = [&](int t) { return code(VC == 8 ? raw[2 * t + c / 4] : raw[t], c & 3); };
                 const uint4 x = {pack_code(val(0), val(1)), pack_code(val(2), val(3)), pack_code(val(4), val(5)), pack_code(val(6), val(7))};
                 *(uint4*)(base + (v_put ^ (c >> 1 << 4)) + c * 128) = x;
             }
