@@ -178,7 +178,8 @@ struct SampleArgs {
     int32_t* tokens; float* logprobs;                                                                     // logprobs may be null
 };
 constexpr int SAMPLE_MOST_VOCAB = 1 << 19;
-// Takes as many rows at once as the workspace holds (45 KB each; the smallest context has 1.5 MB).
+// Takes as many rows at once as the workspace holds (the smallest context has 1.5 MB).
+constexpr int SAMPLE_ROW_BYTES = 47656;   // what a row needs of it
 hipError_t launch_sample(const SampleArgs& a, void* ws, size_t ws_bytes, hipStream_t st);
 
 }  // namespace cake

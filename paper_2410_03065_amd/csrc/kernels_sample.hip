@@ -51,6 +51,7 @@ struct Row {
     Plan plan;
     u64 list[LIST];
 };
+static_assert(sizeof(Row) == SAMPLE_ROW_BYTES);
 
 struct Args {
     const float* logits; int64_t stride; int rows_n, vocab, slices, slice_len;
