@@ -127,7 +127,7 @@ class Q8Batch(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("pool", "block_table", "seq_len", "row_begin")] + \
                [(n, C.c_int32) for n in ("n_seqs", "pages_per_seq", "page_tokens", "scale_tokens", "n_physical_pages", "n_rows", "max_rows",
                                          "max_len")]
-    model = None     # (layers, KV heads, head size) of the pages, where an Engine has described them
+    model = None     # (layers, KV heads, head size, device) of the pages, where an Engine has described them
 
 
 ROPE_LAYOUTS = {"pairs": 0, "halves": 1}
@@ -353,14 +353,14 @@ class Engine:
         if not torch.cuda.is_available():
             raise CakeError(E_STATE, "no GPU: the HIP path cannot run and there is no CPU fallback")
         self.shape = shape
-        self._q8_model = (shape.n_layers, shape.n_kv, shape.head_dim)
         self.dev = torch.device(device)
         torch.cuda.set_device(self.dev)
         self.tdtype = torch.float32 if shape.dtype == "f32" else torch.bfloat16
         self.page_tokens = page_tokens
         self.max_tokens, self.max_chunk = max_tokens, max_chunk
-        self._take_streams(compute_stream)
         self._dev_index = self.dev.index if self.dev.index is not None else torch.cuda.current_device()
+        self._q8_model = (shape.n_layers, shape.n_kv, shape.head_dim, self._dev_index)
+        self._take_streams(compute_stream)
         self._compute_raw = self.compute_stream.cuda_stream
         self._tensors = []
         self.with_head = with_head or (weights is not None and "lm_head" in weights)
@@ -827,9 +827,9 @@ class Engine:
             self._check(rc, what)
 
     def _batch(self, batch):
-        """The batch, or a refusal where it describes pages of another model."""
+        """The batch, or a refusal where it describes pages of another model or on another device."""
         if batch.model is not self._q8_model and batch.model not in (None, self._q8_model):
-            raise CakeError(E_INVAL, "batch: described for (layers, KV heads, head size) %s, not %s" % (batch.model, self._q8_model))
+            raise CakeError(E_INVAL, "batch: described for (layers, KV heads, head size, device) %s, not %s" % (batch.model, self._q8_model))
         return batch
 
     def _operand(self, t, name, dtype, shape=None):
