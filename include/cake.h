@@ -551,7 +551,7 @@ typedef struct {
     const int32_t* block_table; /* device, [n_seqs][pages_per_seq]; entries past a sequence's last page are not read */
     const int32_t* seq_len;     /* device, [n_seqs] */
     const int32_t* row_begin;   /* device, [n_seqs + 1], not decreasing */
-    int32_t n_seqs;
+    int32_t n_seqs;             /* n_seqs * n_kv_heads <= 2^22 */
     int32_t pages_per_seq;
     int32_t page_tokens;        /* a multiple of 64 */
     int32_t scale_tokens;       /* tokens that share a scale: 1, 4, 8, 16, 32 or 64; n_kv_heads * page_tokens / scale_tokens a multiple of 4 */

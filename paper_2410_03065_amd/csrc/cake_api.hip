@@ -1562,7 +1562,7 @@ static int check_q8(cake_ctx* c, const char* what, const cake_q8_batch* b, int l
     const uint64_t page = cake_q8_page_bytes(&c->m, b->page_tokens, b->scale_tokens);
     if (!page) return fail(c, CAKE_E_INVAL, "%s: batch: pages of %d tokens with a scale for %d are not supported", what, b->page_tokens, b->scale_tokens);
     if (off16(b->pool)) return fail(c, CAKE_E_INVAL, "%s: batch: the pool is not 16-byte aligned", what);
-    if (b->n_seqs < 0 || int64_t(b->n_seqs) * c->m.n_kv_heads > (1 << 26) || b->n_rows < 0 || b->n_rows > (1 << 28) || b->pages_per_seq <= 0 || b->n_physical_pages <= 0 ||
+    if (b->n_seqs < 0 || int64_t(b->n_seqs) * c->m.n_kv_heads > Q8_MOST_GROUPS || b->n_rows < 0 || b->n_rows > (1 << 28) || b->pages_per_seq <= 0 || b->n_physical_pages <= 0 ||
         int64_t(b->pages_per_seq) * b->page_tokens > Q8_MOST_TOKENS)
         return fail(c, CAKE_E_INVAL, "%s: batch: %d sequences of %d pages, %d rows, %d pages in the pool", what, b->n_seqs, b->pages_per_seq, b->n_rows, b->n_physical_pages);
     if (b->max_rows < 0 || b->max_len < 0) return fail(c, CAKE_E_INVAL, "%s: batch: negative max_rows or max_len", what);

@@ -158,6 +158,7 @@ hipError_t launch_argmax(const float* v, int n, ArgmaxWs* ws, int32_t* result, h
 
 // ---- a ragged batch over an 8-bit paged cache, one layer (cake_q8_batch) ----
 constexpr int Q8_MOST_TOKENS = 1 << 30;   // a sequence's tokens as the block table can hold them, at most
+constexpr int Q8_MOST_GROUPS = 1 << 22;   // KV heads of a batch's sequences, at most: a launch has under 2^32 threads, up to 512 for each
 struct Q8View {
     unsigned char* base;                          // the layer's first page
     const int32_t *table, *seq_len, *row_begin;   // device: [n_seqs][pages_per_seq], [n_seqs], [n_seqs + 1]
