@@ -1069,12 +1069,19 @@ hipError_t merge_q8(const Q8View& v, int n_q, const KeyRanges& k, const AttnWs& 
 template <typename T, int HD, int NB, int NS>
 hipError_t attention_q8(const T* q, T* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws, hipStream_t st) {
     const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, 2048, ws);
-    // Undivided on eight waves, without a merge, where that fills the compute units once and sequences are not too long for it.  Measured
-    // (us, against four waves, divided, with the merge; 8 KV heads of 128, a token each; sequences x keys): 1 x 300 7.5, 9.0;
-    // 1 x 701 11.1, 9.6; 8 x 300 7.7, 9.5; 8 x 1500 18.9, 14.4; 16 x 1000 15.0, 17.4; 24 x 1500 20.0, 27.1; 32 x 701 13.4, 19.2;
-    // 32 x 4100 53.8, 65.6; 48 x 4100 94.0, 86.6; 64 x 1500 44.7, 50.8; 64 ragged up to 8191 147.7, 132.8; 256 x 300 60.0, 40.8; 33 ragged
-    // ones up to 4099, 20 rows, heads of 64 39.1, 42.4.
-    const int64_t most_steps = k.groups <= 288 ? std::min<int64_t>(130, 12 + k.groups * k.groups / 550) : k.groups <= 512 ? 50 : 0;
+    // Undivided on eight waves, without a merge, where sequences are not too long for it: one such workgroup fills a compute unit, so the
+    // steps that may be walked by one grow with the share of the 256 units that the last of up to two rounds fills.  Measured (us,
+    // against four waves, divided, with the merge; a token each, 8 KV heads of 128, then of 64; sequences x keys): 1 x 300 7.5, 9.0;
+    // 1 x 701 11.1, 9.6; 8 x 1500 18.9, 14.4; 16 x 2000 23.1, 24.7 and 16.8, 17.1; 16 x 5000 54.9, 46.9 and 34.5, 26.5;
+    // 24 x 4100 47.2, 53.8 and 32.9, 32.7; 32 x 2000 31.3, 38.0 and 17.4, 21.6; 32 x 4100 56.5, 66.5 and 34.3, 39.5;
+    // 33 x 300 14.7, 14.7 and 8.1, 10.7; 33 x 2000 49.3, 41.1 and 24.3, 23.7; 33 x 4100 89.8, 69.3 and 45.6, 41.4; 36 x 1500 39.6, 35.0 and
+    // 19.9, 20.8; 48 x 1000 31.0, 33.5 and 16.1, 21.2; 48 x 3000 74.5, 69.2 and 38.5, 41.5; 64 x 4100 107.6, 116.3 and 59.0, 66.0.
+    // Longer ones of equal length gain too (32 x 8191 105, 114), ragged ones lose what the longest takes alone: 32 of 500 to 4100 44.0,
+    // 44.1, to 8191 84.5, 86.0 and 57.9, 51.6, to 30000 284, 238 and 194, 134; hence no more than 12 + 256 * 256 / 550 steps.
+    // Two workgroups of tiles of 16 rows, heads of 64 and two-byte elements fit a unit: 50 steps in a second round that is hardly filled.
+    constexpr bool PAIRS = HD == 64 && NB == 1 && Terms<T>::Q == 1;
+    const int64_t last = k.groups % 256 ? k.groups % 256 : 256, by_fill = 12 + last * last / 550;
+    const int64_t most_steps = k.groups > 512 ? 0 : PAIRS && k.groups > 256 ? std::max<int64_t>(50, by_fill) : by_fill;
     if (k.steps <= most_steps) {
         hipLaunchKernelGGL((attention_q8_kernel<T, HD, NB, NS, 8>), dim3(unsigned(k.groups)), dim3(512), 0, st, q, out, ws.part, v, n_q, window, sinks, scale,
                            int(k.steps), 1, k.tiles);
