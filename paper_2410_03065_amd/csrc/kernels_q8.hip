@@ -1037,6 +1037,11 @@ hipError_t append_q8(const float* qkv, T* q, T* values, const Q8View& v, const c
 // 4 steps 158 us, 12 144, 24 133, 32 138, 48 133, 64 149, 129 155; one of 701: 4 steps 10.1, 8 11.2, 24 13.1 without a merge).
 // Tiles of 128 rows: 512, two a compute unit (16 ragged sequences, 128 rows: 256 116 us, 512 81, 1024 87); of 256: 256 (one of
 // 16000 keys: 256 48 us, 512 65).
+// In tiles of 128 and 256 rows the workgroups are those that can have rows: a ragged batch has no more tiles than its rows fill and one for
+// each sequence's last.  Measured (us, as if every sequence had max_rows rows, and so; 8 KV heads of 128, one chunk beside single
+// tokens): 256 rows, three tokens, all at 16000 keys 419, 221; 256 rows at 8000, 15 tokens at 500 to 8191 689, 421; 1024 rows, three
+// tokens at 16000 819, 726; 1024 rows at 8000, three tokens at 500 to 8191 367, 380; 63 tokens 2144, 2144.  Tiles of 16 and 32 rows are many small
+// workgroups, and those without rows count in what a launch takes: 24 rows at 8000, three tokens 32, 41, so there it is all of them.
 struct KeyRanges { int tiles, chunk, splits; int64_t steps, groups; };
 KeyRanges key_ranges(const Q8View& v, int n_q, int rows_per_tile, int width, int max_rows, int max_len, int window, int sinks, int least, int most, int64_t want,
                      const AttnWs& ws) {
@@ -1046,7 +1051,8 @@ KeyRanges key_ranges(const Q8View& v, int n_q, int rows_per_tile, int width, int
     const int64_t seen = std::min<int64_t>(max_len, int64_t(window) + sinks + rows_per_tile / G + 2 * width);
     const int64_t steps = k.steps = seen / width + 1;
     k.groups = int64_t(v.n_seqs) * v.n_kv * k.tiles;
-    int64_t chunk = std::min<int64_t>(std::max<int64_t>(least, (steps * k.groups + want - 1) / want), most);
+    const int64_t busy = rows_per_tile < 128 ? k.groups : v.n_kv * std::min<int64_t>(int64_t(v.n_seqs) * k.tiles, int64_t(v.n_rows) * G / rows_per_tile + v.n_seqs);
+    int64_t chunk = std::min<int64_t>(std::max<int64_t>(least, (steps * busy + want - 1) / want), most);
     chunk = std::max(chunk, steps * k.groups / 16384);        // ranges past a sequence's end cost a little too
     int64_t splits = std::max<int64_t>(1, (steps + chunk - 1) / chunk);
     splits = std::min<int64_t>(splits, int64_t(ws.bytes / (size_t(v.n_rows) * n_q * (v.head_dim + 4) * 4)));
