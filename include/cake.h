@@ -559,7 +559,9 @@ typedef struct {
     int32_t n_rows;             /* rows of the batch's activations */
     int32_t max_rows;           /* most rows of one sequence and ... */
     int32_t max_len;            /* ... most tokens of one: they choose kernels and launch sizes, results depend on them
-                                 * no further than the roundings that cake_op_attention_q8 states (0: unknown) */
+                                 * no further than the roundings that cake_op_attention_q8 states (0: unknown).  They are read when
+                                 * a call is made: one who keeps a description raises them as the sequences grow, and records a
+                                 * graph again, or launches stay as small as they were (right, but slow) */
 } cake_q8_batch;
 
 /* Bytes of one layer page, 0 if the sizes are not supported.  Pure. */
@@ -599,7 +601,7 @@ int32_t cake_rope_init(cake_rope* out, const cake_rope_desc* desc);
  * qkv[n_rows][(n_q + 2 n_kv) head_dim] (device, float32), and the rotated keys and the values go into the pages as codes.  Row i of
  * a sequence's rows is at position seq_len - rows + i.  Rotated in 64 bits and rounded to float32 once; scale and code are
  * float32 quotients, codes rounded half to even.  A block that already holds earlier tokens keeps the larger of its scale and the
- * new tokens'; where that is larger the earlier codes become rint(code * old / new).  A block with an infinity or a NaN gets a
+ * new tokens'; where that is larger the earlier codes become rint(code * (old / new)), a float32 quotient.  A block with an infinity or a NaN gets a
  * NaN scale.  values: device, [n_rows][2 n_kv][head_dim] in the model dtype, what the pages now stand for (K heads, then V heads;
  * NaN where no page could be written), or NULL.  No two sequences may append to one page.  Pointers 16-byte aligned.
  * Errors: CAKE_E_INVAL, CAKE_E_HIP. */
@@ -609,7 +611,8 @@ int32_t cake_op_append_q8(cake_ctx* ctx, const float* qkv, void* q, void* values
  * position p sees keys j <= p, with window > 0 only those with p - j < window or j < sinks.  A row that sees no key is zeros.  Scores,
  * softmax and sums in float32; on the way into the second product bf16 models round a weight times its
  * value's scale to 16 bits, or, with many rows (n_q / n_kv of them a token; heads of 128: more than 96, heads of 64: 512 or more), to 11 bits,
- * and to 2^-28 of the row's largest weight times the largest scale of the key's 64 tokens.
+ * and to 2^-28 of the row's largest weight times the largest scale of the key's 64 tokens (any that a row computed beside this one sees; no
+ * finer than 2^-108 of the largest scale of the keys before).  A batch of a chunk beside many single tokens takes longer than the two in calls of their own.
  * Pointers 16-byte aligned.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
                              const cake_q8_batch* batch);

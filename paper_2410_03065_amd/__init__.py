@@ -850,7 +850,8 @@ class Engine:
     def q8_batch(self, pool, block_table, seq_len, row_begin, *, n_rows, page_tokens, scale_tokens=1, max_rows=0, max_len=0) -> Q8Batch:
         """The description of a batch for op_append_q8 and op_attention_q8 (cake_q8_batch).  pool: uint8 [n_layers *] pages x page
         bytes; block_table: int32 [n_seqs][pages_per_seq]; seq_len: int32 [n_seqs]; row_begin: int32 [n_seqs + 1].  It may be kept
-        and used while the tensors stay; what they hold is read when the work runs."""
+        and used while the tensors stay; what they hold is read when the work runs.  max_rows and max_len are read at each call: raise
+        them (b.max_len = ...) as sequences grow, or launches stay as small as they were."""
         torch = self.torch
         page = q8_page_bytes(self.shape, page_tokens, scale_tokens)
         if pool.numel() == 0 or pool.numel() % (page * self.shape.n_layers):
