@@ -526,9 +526,9 @@ int32_t cake_op_decode_attention(cake_ctx* ctx, const float* q, float* out, int3
 int32_t cake_op_decode_attention_static(cake_ctx* ctx, const float* q, float* out, int32_t layer,
                                         int32_t n_keys, const cake_kv* kv);
 
-/* ---- decoding a batch from an 8-bit cache ------------------------------ */
+/* ---- decoding a batch from a cache in 8 or 4 bits ---------------------- */
 
-/* What follows the first token: a batch of sequences whose KV is kept in 8 bits, appended to and read token by token (or
+/* What follows the first token: a batch of sequences whose KV is kept in 8 or 4 bits, appended to and read token by token (or
  * prompt piece by prompt piece), and the choice of each next token.  All calls are asynchronous on the compute stream, allocate nothing
  * and may be captured into a graph; like all launches of a context they use its workspace, so graphs captured from one
  * context are replayed one after another.
@@ -539,6 +539,9 @@ int32_t cake_op_decode_attention_static(cake_ctx* ctx, const float* q, float* ou
  *     V codes, V scales likewise (V not transposed)
  * value = code * scale, scale = largest magnitude of the block of scale_tokens tokens / 127.  With scale_tokens = 1 the bytes are
  * those of the CAKE_STORE_INT8 image of that layer.
+ * Pages of 4 bits (the calls named q4): codes uint8 [kv_head][token_in_page][head_dim / 2], element 2i in the low half of byte i, two's
+ * complement from -7 to 7, value = code * scale, scale = largest magnitude of the block / 7, cake_q4_page_bytes apart; all else is the
+ * same, and with scale_tokens = 1 the bytes are those of the CAKE_STORE_INT4 image.
  *
  * The arrays of the batch are read on the device when the work runs, so a captured step goes on with what they hold then.
  * Sequence s has seq_len[s] tokens, the new ones included; rows row_begin[s] .. row_begin[s + 1] - 1 of the batch are its LAST
@@ -563,9 +566,11 @@ typedef struct {
                                  * a call is made: one who keeps a description raises them as the sequences grow, and records a
                                  * graph again, or launches stay as small as they were (right, but slow) */
 } cake_q8_batch;
+typedef cake_q8_batch cake_q4_batch;   /* the same, of a pool of 4-bit pages */
 
 /* Bytes of one layer page, 0 if the sizes are not supported.  Pure. */
 uint64_t cake_q8_page_bytes(const cake_model_desc* model, int32_t page_tokens, int32_t scale_tokens);
+uint64_t cake_q4_page_bytes(const cake_model_desc* model, int32_t page_tokens, int32_t scale_tokens);
 
 /* Rotary positions: of each head the first rotary_dim elements turn, in pairs (2i, 2i+1) or (i, i + rotary_dim/2), by position *
  * freq[i]; cosine and sine are multiplied by magnitude. */
@@ -616,6 +621,12 @@ int32_t cake_op_append_q8(cake_ctx* ctx, const float* qkv, void* q, void* values
  * Pointers 16-byte aligned.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
                              const cake_q8_batch* batch);
+/* The two calls on pages of 4 bits: codes rounded to 7 steps of the scale either way, the rest as above.  A code of -8, which append never writes,
+ * counts as what it says.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
+int32_t cake_op_append_q4(cake_ctx* ctx, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope,
+                          const cake_q4_batch* batch);
+int32_t cake_op_attention_q4(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
+                             const cake_q4_batch* batch);
 
 /* The next token of each row of logits (device, float32, rows row_stride elements apart), all arrays device, [rows]:
  *  - temperature T (NULL: 1); T <= 0 or NaN: the likeliest token, lowest id among equals, log-probability 0;
@@ -631,6 +642,34 @@ int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t la
  * rows <= 2^20, vocab <= 2^19, row_stride >= vocab.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_sample(cake_ctx* ctx, const float* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
                        const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tokens, float* logprobs);
+
+/* ---- products with 4-bit weights --------------------------------------- */
+
+/* A projection matrix in 4 bits: weight (n, k) = code * scale[n][k / group].  Codes uint8, rows of (k + 31) / 32 * 16 bytes, element 2i in the low
+ * half of byte i, two's complement from -8 to 7; what a row holds past its last element does not matter.  Scales in the model dtype,
+ * [n][(k + group - 1) / group]; the last group of a row may be short. */
+typedef struct {
+    const void* codes;          /* device, 16-byte aligned */
+    const void* scales;         /* device */
+    int32_t n;                  /* outputs */
+    int32_t k;                  /* inputs, a multiple of 8 */
+    int32_t group;              /* inputs that share a scale: 32, 64 or 128 */
+    int32_t pad_;
+} cake_w4;
+/* Codes and scales of weights w[N][K] (device, model dtype): scale = largest magnitude of the group / 7, rounded to the model dtype, code =
+ * w / scale (a float32 quotient) rounded half to even, from -7 to 7; padding codes are 0.  A group with an infinity or a NaN gets a NaN scale.
+ * values: device, [N][K] in the model dtype, what codes and scales stand for, rounded once, or NULL.  Pointers 16-byte aligned (scales: an element).
+ * Asynchronous on the compute stream like all calls here; they allocate nothing and may be captured into a graph.
+ * Errors: CAKE_E_INVAL, CAKE_E_HIP. */
+int32_t cake_op_pack_w4(cake_ctx* ctx, const void* w, void* codes, void* scales, void* values, int32_t N, int32_t K, int32_t group);
+/* The products of cake_op_gemm, cake_op_gemm_residual and cake_op_gemm_swiglu with such weights: a[M][K] (device, model dtype, 16-byte aligned),
+ *   out[M][N] (float32) = a w^T;   x[M][N] (float32) += a w^T;   out[M][N] (model dtype) = silu(a gate^T) * (a up^T), gate and up of one size.
+ * Activations and codes are multiplied as they are and added up in float32; a group's sum is multiplied by its scale in float32.  The sum over
+ * the groups may be taken in another order for other M.  M <= 2^20; N and K <= 2^20.  The result must not overlap what is read.
+ * Errors: CAKE_E_INVAL, CAKE_E_HIP. */
+int32_t cake_op_gemm_w4(cake_ctx* ctx, const void* a, const cake_w4* w, float* out, int32_t M);
+int32_t cake_op_gemm_w4_residual(cake_ctx* ctx, const void* a, const cake_w4* w, float* x, int32_t M);
+int32_t cake_op_gemm_w4_swiglu(cake_ctx* ctx, const void* a, const cake_w4* gate, const cake_w4* up, void* out, int32_t M);
 
 #ifdef __cplusplus
 }

@@ -1,6 +1,6 @@
-"""Decoding a batch from an 8-bit paged cache, in 64 bits: the definitions that the calls of include/cake.h state
-(cake_op_append_q8, cake_op_attention_q8, cake_op_sample), written from their formulas with NumPy, a sequence, a head and a
-row at a time."""
+"""Decoding a batch from a paged cache in 8 or 4 bits, in 64 bits: the definitions that the calls of include/cake.h state
+(cake_op_append_q8, cake_op_attention_q8, their q4 forms, cake_op_sample, cake_op_pack_w4, the cake_op_gemm_w4 products), written from their
+formulas with NumPy, a sequence, a head and a row at a time."""
 from __future__ import annotations
 
 import math
@@ -48,16 +48,18 @@ def rotate(x, pos, freq, magnitude, layout):
 
 class Pages:
     """The 8-bit pages of one layer, in the layout of the pool: codes int8 [page][K|V][head][token][hd], scales float32
-    [page][K|V][head][token / block]."""
+    [page][K|V][head][token / block].  bits=4: of 4-bit pages, whose bytes hold two codes each (self.codes: one each, as for 8)."""
 
-    def __init__(self, n_pages, n_kv, page_tokens, hd, block):
-        self.pt, self.block, self.n_kv, self.hd = page_tokens, block, n_kv, hd
+    def __init__(self, n_pages, n_kv, page_tokens, hd, block, bits=8):
+        self.pt, self.block, self.n_kv, self.hd, self.bits = page_tokens, block, n_kv, hd, bits
+        self.top = 127 if bits == 8 else 7
         self.codes = np.zeros((n_pages, 2, n_kv, page_tokens, hd), np.int8)
         self.scales = np.zeros((n_pages, 2, n_kv, page_tokens // block), np.float32)
 
     def bytes(self):
         n = len(self.codes)
-        return np.concatenate([np.concatenate([self.codes[:, w].reshape(n, -1).view(np.uint8), self.scales[:, w].reshape(n, -1).view(np.uint8)], axis=1)
+        raw = (lambda c: c) if self.bits == 8 else two_a_byte
+        return np.concatenate([np.concatenate([raw(self.codes[:, w].reshape(n, -1)).view(np.uint8), self.scales[:, w].reshape(n, -1).view(np.uint8)], axis=1)
                                for w in (0, 1)], axis=1)
 
     def take(self, raw):
@@ -65,8 +67,9 @@ class Pages:
         at, n = 0, len(raw)
         raw = np.ascontiguousarray(raw)
         for w in (0, 1):
-            c = self.n_kv * self.pt * self.hd
-            self.codes[:, w] = raw[:, at:at + c].view(np.int8).reshape(n, self.n_kv, self.pt, self.hd)
+            c = self.n_kv * self.pt * self.hd * self.bits // 8
+            codes = raw[:, at:at + c].view(np.int8) if self.bits == 8 else one_each(raw[:, at:at + c])
+            self.codes[:, w] = codes.reshape(n, self.n_kv, self.pt, self.hd)
             at += c
             c = self.n_kv * (self.pt // self.block) * 4
             self.scales[:, w] = np.ascontiguousarray(raw[:, at:at + c]).view(np.float32).reshape(n, self.n_kv, -1)
@@ -77,9 +80,9 @@ class Pages:
         """Whole pages from values x [page][head][token][hd]."""
         n = len(x)
         b = x.astype(np.float32).reshape(n, self.n_kv, self.pt // self.block, self.block * self.hd)
-        s = np.abs(b).max(axis=3) / np.float32(127)
+        s = np.abs(b).max(axis=3) / np.float32(self.top)
         self.scales[:, which] = s
-        self.codes[:, which] = quantise(b, s[..., None]).reshape(n, self.n_kv, self.pt, self.hd)
+        self.codes[:, which] = quantise(b, s[..., None], self.top).reshape(n, self.n_kv, self.pt, self.hd)
         return self
 
     def values(self, which, pages, n):
@@ -88,11 +91,24 @@ class Pages:
         return c.transpose(1, 0, 2, 3).reshape(self.n_kv, -1, self.hd)[:, :n]
 
 
-def quantise(x, scale):
+def quantise(x, scale, top=127):
     """float32 in, whole numbers out."""
     with np.errstate(divide="ignore", invalid="ignore"):
-        c = np.clip(np.rint(x / scale), -127, 127)
+        c = np.clip(np.rint(x / scale), -top, top)
     return np.where(scale > 0, c, 0)
+
+
+def two_a_byte(codes):
+    """Whole numbers from -8 to 7, [..., 2n] -> uint8 [..., n], the first of two in the low half."""
+    c = np.asarray(codes).astype(np.int64) % 16
+    return (c[..., 0::2] + 16 * c[..., 1::2]).astype(np.uint8)
+
+
+def one_each(raw):
+    """The codes of bytes [..., n] -> int8 [..., 2n]."""
+    b = np.asarray(raw).astype(np.int64)
+    both = np.stack([b % 16, b // 16], axis=-1).reshape(*b.shape[:-1], -1)
+    return np.where(both > 7, both - 16, both).astype(np.int8)
 
 
 def append(pages, qkv, table, lens, begin, n_q, freq, magnitude, layout):
@@ -118,7 +134,7 @@ def append(pages, qkv, table, lens, begin, n_q, freq, magnitude, layout):
             if page < 0 or page >= len(pages.codes):
                 continue
             top = np.max([np.abs(v).max(axis=2) for _, _, v in items], axis=0)
-            scale = np.where(np.isfinite(top), top / np.float32(127), np.float32(np.nan)).astype(np.float32)
+            scale = np.where(np.isfinite(top), top / np.float32(pages.top), np.float32(np.nan)).astype(np.float32)
             older = items[0][0] - b * block
             if older > 0:
                 had = pages.scales[page, :, :, slot].copy()
@@ -126,11 +142,11 @@ def append(pages, qkv, table, lens, begin, n_q, freq, magnitude, layout):
                 with np.errstate(divide="ignore", invalid="ignore"):
                     ratio = np.where(scale > 0, had / scale, np.float32(1)).astype(np.float32)
                 at = slice(b * block % pt, b * block % pt + older)
-                moved = np.clip(np.rint(pages.codes[page, :, :, at].astype(np.float32) * ratio[..., None, None]), -127, 127)
+                moved = np.clip(np.rint(pages.codes[page, :, :, at].astype(np.float32) * ratio[..., None, None]), -pages.top, pages.top)
                 pages.codes[page, :, :, at] = np.where(ratio[..., None, None] < 1, moved, pages.codes[page, :, :, at])
             pages.scales[page, :, :, slot] = scale
             for pos, row, v in items:
-                c = quantise(v, scale[..., None])
+                c = quantise(v, scale[..., None], pages.top)
                 pages.codes[page, :, :, pos % pt] = c
                 values[row] = (c * scale[..., None].astype(np.float64)).reshape(2 * n_kv, hd)
     return q, values
@@ -209,3 +225,38 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
         tokens.append(int(ids[at]))
         logprobs.append(z[ids[at]] - math.log(run[-1]))
     return np.array(tokens, np.int32), np.array(logprobs)
+
+
+def round_to(x, kind):
+    """float32 values rounded to the model's element type ("f32" or "bf16"), as float32."""
+    x = np.asarray(x, np.float32)
+    if kind == "f32":
+        return x
+    bits = x.view(np.uint32).astype(np.uint64)
+    up = ((bits + 0x7FFF + ((bits >> 16) & 1)) & 0xFFFF0000).astype(np.uint32).view(np.float32)
+    return np.where(np.isnan(x), np.float32(np.nan), up)
+
+
+def pack_w4(w, group, kind):
+    """(codes as bytes [N][(K + 31) // 32 * 16], scales [N][groups] float32, values [N][K] float64) of weights [N][K]."""
+    w = np.asarray(w, np.float32)
+    N, K = w.shape
+    codes, scales = np.zeros((N, (K + 31) // 32 * 32)), []
+    for k in range(0, K, group):
+        part = w[:, k:k + group]
+        top = np.abs(part).max(axis=1)
+        with np.errstate(invalid="ignore"):
+            s = round_to(np.where(np.isfinite(top), top / np.float32(7), np.float32(np.nan)), kind)
+        codes[:, k:k + part.shape[1]] = quantise(part, s[:, None], 7)
+        scales.append(s)
+    raw, scales = two_a_byte(codes), np.stack(scales, axis=1)
+    return raw, scales, w4_values(raw, scales, K, group)
+
+
+def w4_values(raw, scales, K, group):
+    """The weights [N][K], float64, that bytes and scales stand for."""
+    return one_each(raw)[:, :K].astype(np.float64) * np.repeat(np.asarray(scales, np.float64), group, axis=1)[:, :K]
+
+
+def silu_product(gate, up):
+    return gate / (1 + np.exp(-gate)) * up

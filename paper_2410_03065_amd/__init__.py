@@ -34,6 +34,7 @@ EXPORTS = [
     "cake_op_attention", "cake_profile_enable", "cake_profile_read", "cake_adaptive_serve", "cake_first_token",
     "cake_op_decode_attention", "cake_op_decode_attention_static", "cake_set_traces", "cake_store_image_bytes", "cake_write_store", "cake_prefix_keys", "cake_prefix_lookup",
     "cake_q8_page_bytes", "cake_rope_init", "cake_op_append_q8", "cake_op_attention_q8", "cake_op_sample",
+    "cake_q4_page_bytes", "cake_op_append_q4", "cake_op_attention_q4", "cake_op_pack_w4", "cake_op_gemm_w4", "cake_op_gemm_w4_residual", "cake_op_gemm_w4_swiglu",
 ]
 STORE_RAW, STORE_INT8, STORE_INT4 = 0, 1, 2
 STORE_PINNED, STORE_FILE = 0, 1
@@ -123,11 +124,19 @@ class Tuning(C.Structure):
 
 
 class Q8Batch(C.Structure):
-    """cake_q8_batch; Engine.q8_batch makes one and keeps the tensors it points to."""
+    """cake_q8_batch; Engine.q8_batch makes one and keeps the tensors it points to.  Engine.q4_batch: the same of a pool of 4-bit pages."""
     _fields_ = [(n, C.c_void_p) for n in ("pool", "block_table", "seq_len", "row_begin")] + \
                [(n, C.c_int32) for n in ("n_seqs", "pages_per_seq", "page_tokens", "scale_tokens", "n_physical_pages", "n_rows", "max_rows",
                                          "max_len")]
-    model = None     # (layers, KV heads, head size, device) of the pages, where an Engine has described them
+    model = None     # (layers, KV heads, head size, device) of the pages, where an Engine has described them; of 4-bit ones (.., "4 bits")
+
+
+class W4(C.Structure):
+    """cake_w4: a projection in 4 bits.  Engine.w4 describes one and Engine.pack_w4 makes one; both keep its tensors: codes uint8
+    [n][(k + 31) // 32 * 16], scales [n][groups]."""
+    _fields_ = [(n, C.c_void_p) for n in ("codes_at", "scales_at")] + [(n, C.c_int32) for n in ("n", "k", "group", "pad_")]
+    codes = scales = None
+    model = None     # (element type, device), where an Engine has described it
 
 
 ROPE_LAYOUTS = {"pairs": 0, "halves": 1}
@@ -196,6 +205,13 @@ def load_library():
         "cake_rope_init": (i32, [P(Rope), P(RopeDesc)]),
         "cake_op_append_q8": (i32, [vp, vp, vp, vp, i32, P(Rope), P(Q8Batch)]),
         "cake_op_attention_q8": (i32, [vp, vp, vp, i32, i32, i32, P(Q8Batch)]),
+        "cake_q4_page_bytes": (u64, [P(ModelDesc), i32, i32]),
+        "cake_op_append_q4": (i32, [vp, vp, vp, vp, i32, P(Rope), P(Q8Batch)]),
+        "cake_op_attention_q4": (i32, [vp, vp, vp, i32, i32, i32, P(Q8Batch)]),
+        "cake_op_pack_w4": (i32, [vp, vp, vp, vp, vp, i32, i32, i32]),
+        "cake_op_gemm_w4": (i32, [vp, vp, P(W4), vp, i32]),
+        "cake_op_gemm_w4_residual": (i32, [vp, vp, P(W4), vp, i32]),
+        "cake_op_gemm_w4_swiglu": (i32, [vp, vp, P(W4), P(W4), vp, i32]),
         "cake_op_sample": (i32, [vp, vp, C.c_int64, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -291,6 +307,14 @@ def q8_page_bytes(shape, page_tokens, scale_tokens=1) -> int:
     return n
 
 
+def q4_page_bytes(shape, page_tokens, scale_tokens=1) -> int:
+    """Bytes of one layer page of a 4-bit cache (cake_q4_page_bytes)."""
+    n = int(load_library().cake_q4_page_bytes(C.byref(model_desc(shape)), page_tokens, scale_tokens))
+    if n == 0:
+        raise CakeError(E_INVAL, "cake_q4_page_bytes: pages of %d tokens with a scale for %d" % (page_tokens, scale_tokens))
+    return n
+
+
 def rope(theta, rotary_dim, layout="pairs", scaling=None) -> Rope:
     """Rotary positions (cake_rope_init).  scaling: None, ("linear", factor), ("bands", factor, low, high, original_tokens) or
     ("ramp", factor, original_tokens, high, low); see cake_rope_scaling."""
@@ -340,8 +364,8 @@ class Engine:
     """Owns the device tensors (weights in ABI layout, KV pool, block tables), the pinned
     store and the two streams, and forwards to the C ABI.  The op_* calls wait for what torch's current
     stream was given before them (their operands come from there); the others do not: synchronise
-    after torch has written to the pool.  op_append_q8, op_attention_q8 and op_sample return before their work is done: it runs
-    in order with torch's current stream, without a wait where that is the compute stream.
+    after torch has written to the pool.  op_append_q8, op_attention_q8, their q4 forms, op_sample, pack_w4 and the op_gemm_w4 calls return
+    before their work is done: it runs in order with torch's current stream, without a wait where that is the compute stream.
     compute_stream: a torch stream of the default priority to use as the compute stream (None: one of the engine's own).
     An engine on torch's default stream runs such calls with the least delay, but they cannot be captured into a graph."""
 
@@ -360,6 +384,8 @@ class Engine:
         self.max_tokens, self.max_chunk = max_tokens, max_chunk
         self._dev_index = self.dev.index if self.dev.index is not None else torch.cuda.current_device()
         self._q8_model = (shape.n_layers, shape.n_kv, shape.head_dim, self._dev_index)
+        self._q4_model = self._q8_model + ("4 bits",)
+        self._w4_model = (shape.dtype, self._dev_index)
         self._take_streams(compute_stream)
         self._compute_raw = self.compute_stream.cuda_stream
         self._tensors = []
@@ -814,7 +840,7 @@ class Engine:
         self.sync()
         return out
 
-    # -- a ragged batch over an 8-bit cache ---------------------------------------------
+    # -- a ragged batch over a cache in 8 or 4 bits ---------------------------------------------
     def _in_order(self, fn, what, *args):
         """A call whose work is to run between what torch's current stream has and what it gets next."""
         if self.torch._C._cuda_getCurrentRawStream(self._dev_index) == self._compute_raw:
@@ -829,10 +855,11 @@ class Engine:
         if rc != OK:
             self._check(rc, what)
 
-    def _batch(self, batch):
-        """The batch, or a refusal where it describes pages of another model or on another device."""
-        if batch.model is not self._q8_model and batch.model not in (None, self._q8_model):
-            raise CakeError(E_INVAL, "batch: described for (layers, KV heads, head size, device) %s, not %s" % (batch.model, self._q8_model))
+    def _batch(self, batch, model=None):
+        """The batch, or a refusal where it describes pages of another model, of other codes (model: None, 8-bit ones) or on another device."""
+        model = model or self._q8_model
+        if batch.model is not model and batch.model not in (None, model):
+            raise CakeError(E_INVAL, "batch: described for (layers, KV heads, head size, device) %s, not %s" % (batch.model, model))
         return batch
 
     def _operand(self, t, name, dtype, shape=None):
@@ -847,43 +874,128 @@ class Engine:
         return self.torch.zeros((self.shape.n_layers, n_pages, q8_page_bytes(self.shape, page_tokens, scale_tokens)),
                                 dtype=self.torch.uint8, device=self.dev)
 
+    def new_q4_pool(self, n_pages, page_tokens, scale_tokens=1):
+        """A pool of 4-bit pages, zeros: uint8 [n_layers][n_pages][page bytes]."""
+        return self.torch.zeros((self.shape.n_layers, n_pages, q4_page_bytes(self.shape, page_tokens, scale_tokens)),
+                                dtype=self.torch.uint8, device=self.dev)
+
+    def _describe(self, what, page, model, pool, block_table, seq_len, row_begin, n_rows, page_tokens, scale_tokens, max_rows, max_len):
+        torch = self.torch
+        if pool.numel() == 0 or pool.numel() % (page * self.shape.n_layers):
+            raise CakeError(E_INVAL, "%s: a pool of %d bytes for %d layers of pages of %d" % (what, pool.numel(), self.shape.n_layers, page))
+        if block_table.dim() != 2:
+            raise CakeError(E_INVAL, "%s: block_table must have a row per sequence" % what)
+        n = block_table.shape[0]
+        b = Q8Batch(self._operand(pool, "pool", torch.uint8), self._operand(block_table, "block_table", torch.int32),
+                    self._operand(seq_len, "seq_len", torch.int32, (n,)), self._operand(row_begin, "row_begin", torch.int32, (n + 1,)),
+                    n, block_table.shape[1], page_tokens, scale_tokens, pool.numel() // (page * self.shape.n_layers), n_rows, max_rows, max_len)
+        b.tensors, b.model = (pool, block_table, seq_len, row_begin), model
+        return b
+
     def q8_batch(self, pool, block_table, seq_len, row_begin, *, n_rows, page_tokens, scale_tokens=1, max_rows=0, max_len=0) -> Q8Batch:
         """The description of a batch for op_append_q8 and op_attention_q8 (cake_q8_batch).  pool: uint8 [n_layers *] pages x page
         bytes; block_table: int32 [n_seqs][pages_per_seq]; seq_len: int32 [n_seqs]; row_begin: int32 [n_seqs + 1].  It may be kept
         and used while the tensors stay; what they hold is read when the work runs.  max_rows and max_len are read at each call: raise
         them (b.max_len = ...) as sequences grow, or launches stay as small as they were."""
-        torch = self.torch
-        page = q8_page_bytes(self.shape, page_tokens, scale_tokens)
-        if pool.numel() == 0 or pool.numel() % (page * self.shape.n_layers):
-            raise CakeError(E_INVAL, "q8_batch: a pool of %d bytes for %d layers of pages of %d" % (pool.numel(), self.shape.n_layers, page))
-        if block_table.dim() != 2:
-            raise CakeError(E_INVAL, "q8_batch: block_table must have a row per sequence")
-        n = block_table.shape[0]
-        b = Q8Batch(self._operand(pool, "pool", torch.uint8), self._operand(block_table, "block_table", torch.int32),
-                    self._operand(seq_len, "seq_len", torch.int32, (n,)), self._operand(row_begin, "row_begin", torch.int32, (n + 1,)),
-                    n, block_table.shape[1], page_tokens, scale_tokens, pool.numel() // (page * self.shape.n_layers), n_rows, max_rows, max_len)
-        b.tensors, b.model = (pool, block_table, seq_len, row_begin), self._q8_model
-        return b
+        return self._describe("q8_batch", q8_page_bytes(self.shape, page_tokens, scale_tokens), self._q8_model, pool, block_table, seq_len, row_begin, n_rows,
+                              page_tokens, scale_tokens, max_rows, max_len)
+
+    def q4_batch(self, pool, block_table, seq_len, row_begin, *, n_rows, page_tokens, scale_tokens=1, max_rows=0, max_len=0) -> Q8Batch:
+        """The description of a batch over 4-bit pages for op_append_q4 and op_attention_q4, otherwise as q8_batch."""
+        return self._describe("q4_batch", q4_page_bytes(self.shape, page_tokens, scale_tokens), self._q4_model, pool, block_table, seq_len, row_begin, n_rows,
+                              page_tokens, scale_tokens, max_rows, max_len)
+
+    def _append(self, fn, what, model, qkv, layer, batch, rope, q, want_values):
+        s, n = self.shape, self._batch(batch, model).n_rows
+        if q is None:
+            q = self.torch.empty((s.n_q, n, s.head_dim), dtype=self.tdtype, device=self.dev)
+        values = self.torch.empty((n, 2 * s.n_kv, s.head_dim), dtype=self.tdtype, device=self.dev) if want_values else None
+        self._in_order(fn, what, self._operand(qkv, "qkv", self.torch.float32, (n, (s.n_q + 2 * s.n_kv) * s.head_dim)),
+                       self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)), values.data_ptr() if want_values else None, layer, rope, batch)
+        return (q, values) if want_values else q
 
     def op_append_q8(self, qkv, layer, batch, rope, q=None, want_values=False):
         """qkv float32 [n_rows][(n_q + 2 n_kv) hd] -> q [n_q][n_rows][hd], rotated; keys and values into the pages.  want_values:
         (q, values [n_rows][2 n_kv][hd] as the pages now hold them)."""
-        s, n = self.shape, self._batch(batch).n_rows
-        if q is None:
-            q = self.torch.empty((s.n_q, n, s.head_dim), dtype=self.tdtype, device=self.dev)
-        values = self.torch.empty((n, 2 * s.n_kv, s.head_dim), dtype=self.tdtype, device=self.dev) if want_values else None
-        self._in_order(self.lib.cake_op_append_q8, "cake_op_append_q8",
-                       self._operand(qkv, "qkv", self.torch.float32, (n, (s.n_q + 2 * s.n_kv) * s.head_dim)),
-                       self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)), values.data_ptr() if want_values else None, layer, rope, batch)
-        return (q, values) if want_values else q
+        return self._append(self.lib.cake_op_append_q8, "cake_op_append_q8", self._q8_model, qkv, layer, batch, rope, q, want_values)
+
+    def op_append_q4(self, qkv, layer, batch, rope, q=None, want_values=False):
+        """op_append_q8 into pages of 4 bits (cake_op_append_q4)."""
+        return self._append(self.lib.cake_op_append_q4, "cake_op_append_q4", self._q4_model, qkv, layer, batch, rope, q, want_values)
+
+    def _attention(self, fn, what, model, q, layer, batch, window, sinks, out):
+        s, n = self.shape, self._batch(batch, model).n_rows
+        if out is None:
+            out = self.torch.empty((n, s.n_q * s.head_dim), dtype=self.tdtype, device=self.dev)
+        self._in_order(fn, what, self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)),
+                       self._operand(out, "out", self.tdtype, (n, s.n_q * s.head_dim)), layer, window, sinks, batch)
+        return out
 
     def op_attention_q8(self, q, layer, batch, window=0, sinks=0, out=None):
         """q [n_q][n_rows][hd] -> [n_rows][n_q * hd] (cake_op_attention_q8)."""
-        s, n = self.shape, self._batch(batch).n_rows
+        return self._attention(self.lib.cake_op_attention_q8, "cake_op_attention_q8", self._q8_model, q, layer, batch, window, sinks, out)
+
+    def op_attention_q4(self, q, layer, batch, window=0, sinks=0, out=None):
+        """op_attention_q8 over pages of 4 bits (cake_op_attention_q4)."""
+        return self._attention(self.lib.cake_op_attention_q4, "cake_op_attention_q4", self._q4_model, q, layer, batch, window, sinks, out)
+
+    # -- products with 4-bit weights ------------------------------------------------------
+    def w4(self, codes, scales, k, group=128) -> W4:
+        """The description of a projection in 4 bits (cake_w4): codes uint8 [n][(k + 31) // 32 * 16], two a byte; scales [n][(k + group - 1) // group]
+        in the model's type.  It may be kept and used while the tensors stay."""
+        if group not in (32, 64, 128) or k <= 0 or k % 8 or codes.dim() != 2 or codes.shape[0] == 0:
+            raise CakeError(E_INVAL, "w4: codes %s for %d inputs, a scale for %d: rows of (k + 31) // 32 * 16 bytes, k by eights and groups of 32, 64 or 128 are needed" % (
+                tuple(codes.shape), k, group))
+        n = codes.shape[0]
+        w = W4(self._operand(codes, "codes", self.torch.uint8, (n, (k + 31) // 32 * 16)), self._operand(scales, "scales", self.tdtype, (n, (k + group - 1) // group)),
+               n, k, group)
+        w.codes, w.scales, w.model = codes, scales, self._w4_model
+        return w
+
+    def pack_w4(self, w, group=128, want_values=False):
+        """w [n][k] of the model's type -> its projection in 4 bits (cake_op_pack_w4).  want_values: (packed, values [n][k] that it stands for)."""
+        torch = self.torch
+        if w.dim() != 2 or w.shape[0] == 0 or w.shape[1] == 0 or w.shape[1] % 8 or group not in (32, 64, 128):
+            raise CakeError(E_INVAL, "pack_w4: weights %s, a scale for %d: inputs by eights and groups of 32, 64 or 128 are needed" % (tuple(w.shape), group))
+        n, k = w.shape
+        at = self._operand(w, "w", self.tdtype)
+        packed = self.w4(torch.empty((n, (k + 31) // 32 * 16), dtype=torch.uint8, device=self.dev),
+                         torch.empty((n, (k + group - 1) // group), dtype=self.tdtype, device=self.dev), k, group)
+        values = torch.empty((n, k), dtype=self.tdtype, device=self.dev) if want_values else None
+        self._in_order(self.lib.cake_op_pack_w4, "cake_op_pack_w4", at, packed.codes_at, packed.scales_at, values.data_ptr() if want_values else None, n, k, group)
+        return (packed, values) if want_values else packed
+
+    def _w4(self, w):
+        """The projection, or a refusal where it is of another element type or on another device."""
+        if w.model is not self._w4_model and w.model not in (None, self._w4_model):
+            raise CakeError(E_INVAL, "w4: described for (element type, device) %s, not %s" % (w.model, self._w4_model))
+        return w
+
+    def _activations(self, a, w):
+        if a.dim() != 2:
+            raise CakeError(E_INVAL, "a: [rows][%d] is needed, got %s" % (w.k, tuple(a.shape)))
+        return self._operand(a, "a", self.tdtype, (a.shape[0], w.k)), a.shape[0]
+
+    def op_gemm_w4(self, a, w, out=None):
+        """a [rows][k] times a projection in 4 bits -> float32 [rows][n] (cake_op_gemm_w4)."""
+        at, rows = self._activations(a, self._w4(w))
         if out is None:
-            out = self.torch.empty((n, s.n_q * s.head_dim), dtype=self.tdtype, device=self.dev)
-        self._in_order(self.lib.cake_op_attention_q8, "cake_op_attention_q8", self._operand(q, "q", self.tdtype, (s.n_q, n, s.head_dim)),
-                       self._operand(out, "out", self.tdtype, (n, s.n_q * s.head_dim)), layer, window, sinks, batch)
+            out = self.torch.empty((rows, w.n), dtype=self.torch.float32, device=self.dev)
+        self._in_order(self.lib.cake_op_gemm_w4, "cake_op_gemm_w4", at, w, self._operand(out, "out", self.torch.float32, (rows, w.n)), rows)
+        return out
+
+    def op_gemm_w4_residual(self, a, w, x):
+        """x (float32 [rows][n]) += a times a projection in 4 bits; returns x (cake_op_gemm_w4_residual)."""
+        at, rows = self._activations(a, self._w4(w))
+        self._in_order(self.lib.cake_op_gemm_w4_residual, "cake_op_gemm_w4_residual", at, w, self._operand(x, "x", self.torch.float32, (rows, w.n)), rows)
+        return x
+
+    def op_gemm_w4_swiglu(self, a, gate, up, out=None):
+        """silu(a gate^T) * (a up^T) -> [rows][n] of the model's type (cake_op_gemm_w4_swiglu)."""
+        at, rows = self._activations(a, self._w4(gate))
+        if out is None:
+            out = self.torch.empty((rows, gate.n), dtype=self.tdtype, device=self.dev)
+        self._in_order(self.lib.cake_op_gemm_w4_swiglu, "cake_op_gemm_w4_swiglu", at, gate, self._w4(up), self._operand(out, "out", self.tdtype, (rows, gate.n)), rows)
         return out
 
     def op_sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None):

@@ -1543,7 +1543,7 @@ int32_t cake_op_decode_attention_static(cake_ctx* c, const float* q, float* out,
     return CAKE_OK;
 }
 
-// ---- a ragged batch over an 8-bit cache ---------------------------------------------------
+// ---- a ragged batch over a cache in 8 or 4 bits ---------------------------------------------------
 // The context's device as the current one while a call lasts (its streams and memory belong to it).
 struct OnDevice {
     int before = -1;
@@ -1556,10 +1556,10 @@ struct OnDevice {
 static bool off16(const void* p) { return (uintptr_t(p) & 15) != 0; }
 
 // Checks what the host can see of a batch (its arrays are read on the device) and lays out the view of one layer.
-static int check_q8(cake_ctx* c, const char* what, const cake_q8_batch* b, int layer, Q8View* v, int* max_rows, int* max_len) {
+static int check_batch(cake_ctx* c, const char* what, int bits, const cake_q8_batch* b, int layer, Q8View* v, int* max_rows, int* max_len) {
     if (layer < 0 || layer >= c->m.n_layers) return fail(c, CAKE_E_INVAL, "%s: layer %d of %d", what, layer, c->m.n_layers);
     if (!b || !b->pool || (b->n_seqs > 0 && (!b->block_table || !b->seq_len || !b->row_begin))) return fail(c, CAKE_E_INVAL, "%s: batch: null pointer", what);
-    const uint64_t page = cake_q8_page_bytes(&c->m, b->page_tokens, b->scale_tokens);
+    const uint64_t page = bits == 8 ? cake_q8_page_bytes(&c->m, b->page_tokens, b->scale_tokens) : cake_q4_page_bytes(&c->m, b->page_tokens, b->scale_tokens);
     if (!page) return fail(c, CAKE_E_INVAL, "%s: batch: pages of %d tokens with a scale for %d are not supported", what, b->page_tokens, b->scale_tokens);
     if (off16(b->pool)) return fail(c, CAKE_E_INVAL, "%s: batch: the pool is not 16-byte aligned", what);
     if (b->n_seqs < 0 || int64_t(b->n_seqs) * c->m.n_kv_heads > Q8_MOST_GROUPS || b->n_rows < 0 || b->n_rows > (1 << 28) || b->pages_per_seq <= 0 || b->n_physical_pages <= 0 ||
@@ -1568,7 +1568,7 @@ static int check_q8(cake_ctx* c, const char* what, const cake_q8_batch* b, int l
     if (b->max_rows < 0 || b->max_len < 0) return fail(c, CAKE_E_INVAL, "%s: batch: negative max_rows or max_len", what);
     *v = Q8View{};
     v->page_bytes = page; v->half_bytes = page / 2;
-    v->scales_off = size_t(c->m.n_kv_heads) * b->page_tokens * c->m.head_dim;
+    v->scales_off = size_t(c->m.n_kv_heads) * b->page_tokens * (c->m.head_dim * bits / 8);
     v->base = (unsigned char*)b->pool + size_t(layer) * b->n_physical_pages * page;
     v->table = b->block_table; v->seq_len = b->seq_len; v->row_begin = b->row_begin;
     v->n_seqs = b->n_seqs; v->pages_per_seq = b->pages_per_seq; v->page_tokens = b->page_tokens; v->n_phys = b->n_physical_pages;
@@ -1580,33 +1580,46 @@ static int check_q8(cake_ctx* c, const char* what, const cake_q8_batch* b, int l
     return CAKE_OK;
 }
 
-int32_t cake_op_append_q8(cake_ctx* c, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope, const cake_q8_batch* batch) {
+static int append_batch(cake_ctx* c, int bits, const char* what, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope, const cake_q8_batch* batch) {
     if (!c) return CAKE_E_INVAL;
     Q8View v;
     int max_rows, max_len;
-    const int rc = check_q8(c, "op_append_q8", batch, layer, &v, &max_rows, &max_len);
+    const int rc = check_batch(c, what, bits, batch, layer, &v, &max_rows, &max_len);
     if (rc != CAKE_OK) return rc;
     if (!rope || rope->rotary_dim < 2 || rope->rotary_dim > c->m.head_dim || rope->rotary_dim % 2 || (rope->layout != CAKE_ROPE_PAIRS && rope->layout != CAKE_ROPE_HALVES))
-        return fail(c, CAKE_E_INVAL, "op_append_q8: rotary description: null, or not for heads of %d", c->m.head_dim);
+        return fail(c, CAKE_E_INVAL, "%s: rotary description: null, or not for heads of %d", what, c->m.head_dim);
     if (v.n_rows == 0 || v.n_seqs == 0) return CAKE_OK;
-    if (!qkv || !q || off16(qkv) || off16(q) || off16(values)) return fail(c, CAKE_E_INVAL, "op_append_q8: qkv, q or values null or not 16-byte aligned");
+    if (!qkv || !q || off16(qkv) || off16(q) || off16(values)) return fail(c, CAKE_E_INVAL, "%s: qkv, q or values null or not 16-byte aligned", what);
     const OnDevice on(c->device);
-    HIP_TRY(c, launch_append_q8(c->m.dtype, qkv, q, values, v, *rope, c->m.n_q_heads, max_rows, c->cs));
+    HIP_TRY(c, (bits == 8 ? launch_append_q8 : launch_append_q4)(c->m.dtype, qkv, q, values, v, *rope, c->m.n_q_heads, max_rows, c->cs));
     return CAKE_OK;
 }
 
-int32_t cake_op_attention_q8(cake_ctx* c, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks, const cake_q8_batch* batch) {
+static int attention_batch(cake_ctx* c, int bits, const char* what, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks, const cake_q8_batch* batch) {
     if (!c) return CAKE_E_INVAL;
     Q8View v;
     int max_rows, max_len;
-    const int rc = check_q8(c, "op_attention_q8", batch, layer, &v, &max_rows, &max_len);
+    const int rc = check_batch(c, what, bits, batch, layer, &v, &max_rows, &max_len);
     if (rc != CAKE_OK) return rc;
-    if (window < 0 || sinks < 0) return fail(c, CAKE_E_INVAL, "op_attention_q8: window %d, sinks %d", window, sinks);
+    if (window < 0 || sinks < 0) return fail(c, CAKE_E_INVAL, "%s: window %d, sinks %d", what, window, sinks);
     if (v.n_rows == 0 || v.n_seqs == 0) return CAKE_OK;
-    if (!q || !out || off16(q) || off16(out)) return fail(c, CAKE_E_INVAL, "op_attention_q8: q or out null or not 16-byte aligned");
+    if (!q || !out || off16(q) || off16(out)) return fail(c, CAKE_E_INVAL, "%s: q or out null or not 16-byte aligned", what);
     const OnDevice on(c->device);
-    HIP_TRY(c, launch_attention_q8(c->m.dtype, q, out, v, c->m.n_q_heads, max_rows, max_len, window, sinks, AttnWs{c->split.part, c->split.part_bytes, 0}, c->cs));
+    HIP_TRY(c, (bits == 8 ? launch_attention_q8 : launch_attention_q4)(c->m.dtype, q, out, v, c->m.n_q_heads, max_rows, max_len, window, sinks, AttnWs{c->split.part, c->split.part_bytes, 0}, c->cs));
     return CAKE_OK;
+}
+
+int32_t cake_op_append_q8(cake_ctx* c, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope, const cake_q8_batch* batch) {
+    return append_batch(c, 8, "op_append_q8", qkv, q, values, layer, rope, batch);
+}
+int32_t cake_op_append_q4(cake_ctx* c, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope, const cake_q4_batch* batch) {
+    return append_batch(c, 4, "op_append_q4", qkv, q, values, layer, rope, batch);
+}
+int32_t cake_op_attention_q8(cake_ctx* c, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks, const cake_q8_batch* batch) {
+    return attention_batch(c, 8, "op_attention_q8", q, out, layer, window, sinks, batch);
+}
+int32_t cake_op_attention_q4(cake_ctx* c, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks, const cake_q4_batch* batch) {
+    return attention_batch(c, 4, "op_attention_q4", q, out, layer, window, sinks, batch);
 }
 
 int32_t cake_op_sample(cake_ctx* c, const float* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature, const int32_t* top_k,
@@ -1618,6 +1631,49 @@ int32_t cake_op_sample(cake_ctx* c, const float* logits, int64_t row_stride, int
     if (!logits || !u || !tokens) return fail(c, CAKE_E_INVAL, "op_sample: null pointer");
     const OnDevice on(c->device);
     HIP_TRY(c, launch_sample({logits, row_stride, rows, vocab, temperature, top_k, top_p, min_p, u, tokens, logprobs}, c->split.part, c->split.part_bytes, c->cs));
+    return CAKE_OK;
+}
+
+// ---- products with 4-bit weights -----------------------------------------------------------
+static int check_w4(cake_ctx* c, const char* what, const cake_w4* w) {
+    if (!w || !w->codes || !w->scales || off16(w->codes) || uintptr_t(w->scales) % (c->m.dtype == CAKE_F32 ? 4 : 2)) return fail(c, CAKE_E_INVAL, "%s: weights: null or not aligned", what);
+    if (w->n <= 0 || w->n > W4_MOST || w->k <= 0 || w->k > W4_MOST || w->k % 8 || (w->group != 32 && w->group != 64 && w->group != 128))
+        return fail(c, CAKE_E_INVAL, "%s: weights of %d outputs, %d inputs, a scale for %d, are not supported", what, w->n, w->k, w->group);
+    return CAKE_OK;
+}
+
+static int gemm_w4(cake_ctx* c, const char* what, int epi, const void* a, const cake_w4* w, const cake_w4* w2, void* out, int32_t M) {
+    if (!c) return CAKE_E_INVAL;
+    int rc = check_w4(c, what, w);
+    if (rc == CAKE_OK && epi == EPI_SWIGLU) {
+        rc = check_w4(c, what, w2);
+        if (rc == CAKE_OK && (w2->n != w->n || w2->k != w->k || w2->group != w->group)) rc = fail(c, CAKE_E_INVAL, "%s: gate and up of different sizes", what);
+    }
+    if (rc != CAKE_OK) return rc;
+    if (M < 0 || M > W4_MOST) return fail(c, CAKE_E_INVAL, "%s: %d rows", what, M);
+    if (M == 0) return CAKE_OK;
+    if (!a || !out || off16(a) || uintptr_t(out) % (epi == EPI_SWIGLU && c->m.dtype == CAKE_BF16 ? 2 : 4)) return fail(c, CAKE_E_INVAL, "%s: activations or result null or not aligned", what);
+    const OnDevice on(c->device);
+    HIP_TRY(c, launch_gemm_w4(c->m.dtype, epi, a, *w, w2, out, M, c->cs));
+    return CAKE_OK;
+}
+
+int32_t cake_op_gemm_w4(cake_ctx* c, const void* a, const cake_w4* w, float* out, int32_t M) { return gemm_w4(c, "op_gemm_w4", EPI_STORE_F32, a, w, nullptr, out, M); }
+int32_t cake_op_gemm_w4_residual(cake_ctx* c, const void* a, const cake_w4* w, float* x, int32_t M) {
+    return gemm_w4(c, "op_gemm_w4_residual", EPI_RESIDUAL_F32, a, w, nullptr, x, M);
+}
+int32_t cake_op_gemm_w4_swiglu(cake_ctx* c, const void* a, const cake_w4* gate, const cake_w4* up, void* out, int32_t M) {
+    return gemm_w4(c, "op_gemm_w4_swiglu", EPI_SWIGLU, a, gate, up, out, M);
+}
+
+int32_t cake_op_pack_w4(cake_ctx* c, const void* w, void* codes, void* scales, void* values, int32_t N, int32_t K, int32_t group) {
+    if (!c) return CAKE_E_INVAL;
+    const cake_w4 d = {codes, scales, N, K, group, 0};
+    const int rc = check_w4(c, "op_pack_w4", &d);
+    if (rc != CAKE_OK) return rc;
+    if (!w || off16(w) || off16(values)) return fail(c, CAKE_E_INVAL, "op_pack_w4: w or values null or not 16-byte aligned");
+    const OnDevice on(c->device);
+    HIP_TRY(c, launch_pack_w4(c->m.dtype, w, codes, scales, values, N, K, group, c->cs));
     return CAKE_OK;
 }
 

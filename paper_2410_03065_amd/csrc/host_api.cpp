@@ -105,13 +105,17 @@ uint64_t cake_page_image_bytes(const cake_model_desc* model, int32_t page_tokens
     return cake::page_image_bytes(*model, page_tokens);
 }
 
-uint64_t cake_q8_page_bytes(const cake_model_desc* m, int32_t page_tokens, int32_t scale_tokens) {
+static uint64_t quant_page_bytes(const cake_model_desc* m, int32_t page_tokens, int32_t scale_tokens, int bits) {
     if (!m || m->n_kv_heads <= 0 || (m->head_dim != 64 && m->head_dim != 128)) return 0;
     if (page_tokens <= 0 || page_tokens % 64 || scale_tokens <= 0 || scale_tokens == 2 || scale_tokens > 64 || (scale_tokens & (scale_tokens - 1))) return 0;
     const uint64_t scales = uint64_t(m->n_kv_heads) * uint64_t(page_tokens / scale_tokens);
     if (scales % 4) return 0;   // every section begins on 16 bytes
-    return 2 * (uint64_t(m->n_kv_heads) * uint64_t(page_tokens) * uint64_t(m->head_dim) + 4 * scales);
+    return 2 * (uint64_t(m->n_kv_heads) * uint64_t(page_tokens) * uint64_t(m->head_dim * bits / 8) + 4 * scales);
 }
+
+uint64_t cake_q8_page_bytes(const cake_model_desc* m, int32_t page_tokens, int32_t scale_tokens) { return quant_page_bytes(m, page_tokens, scale_tokens, 8); }
+
+uint64_t cake_q4_page_bytes(const cake_model_desc* m, int32_t page_tokens, int32_t scale_tokens) { return quant_page_bytes(m, page_tokens, scale_tokens, 4); }
 
 int32_t cake_rope_init(cake_rope* out, const cake_rope_desc* d) {
     if (!out || !d || d->rotary_dim < 2 || d->rotary_dim > 128 || d->rotary_dim % 2) return CAKE_E_INVAL;

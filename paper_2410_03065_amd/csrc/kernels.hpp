@@ -156,7 +156,7 @@ constexpr int ARGMAX_BLOCKS = 128;
 struct ArgmaxWs { unsigned long long best[ARGMAX_BLOCKS]; unsigned counter; };
 hipError_t launch_argmax(const float* v, int n, ArgmaxWs* ws, int32_t* result, hipStream_t st);
 
-// ---- a ragged batch over an 8-bit paged cache, one layer (cake_q8_batch) ----
+// ---- a ragged batch over a paged cache in 8 or 4 bits, one layer (cake_q8_batch) ----
 constexpr int Q8_MOST_TOKENS = 1 << 30;   // a sequence's tokens as the block table can hold them, at most
 constexpr int Q8_MOST_GROUPS = 1 << 22;   // KV heads of a batch's sequences, at most: a launch has under 2^32 threads, up to 512 for each
 struct Q8View {
@@ -171,6 +171,15 @@ hipError_t launch_append_q8(int dtype, const float* qkv, void* q, void* values, 
 // q[n_q][n_rows][hd] -> out[n_rows][n_q hd]; max_rows and max_len choose kernel and key ranges.
 hipError_t launch_attention_q8(int dtype, const void* q, void* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks,
                                const AttnWs& ws, hipStream_t st);
+hipError_t launch_append_q4(int dtype, const float* qkv, void* q, void* values, const Q8View& v, const cake_rope& rope, int n_q, int max_rows, hipStream_t st);
+hipError_t launch_attention_q4(int dtype, const void* q, void* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks,
+                               const AttnWs& ws, hipStream_t st);
+
+// ---- products with 4-bit weights (cake_w4) ----
+constexpr int W4_MOST = 1 << 20;          // rows, outputs and inputs, at most
+// epi: GemmEpilogue; w2: the up weights of EPI_SWIGLU, of w's sizes.
+hipError_t launch_gemm_w4(int dtype, int epi, const void* a, const cake_w4& w, const cake_w4* w2, void* out, int M, hipStream_t st);
+hipError_t launch_pack_w4(int dtype, const void* w, void* codes, void* scales, void* values, int N, int K, int group, hipStream_t st);
 
 // ---- the next token of each row of logits ----
 struct SampleArgs {

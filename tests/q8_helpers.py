@@ -1,4 +1,4 @@
-"""What the tests of the 8-bit batch calls share: a small engine and a ragged batch with scattered pages."""
+"""What the tests of the batch calls share: a small engine and a ragged batch with scattered pages of 8 (or 4) bits."""
 import numpy as np
 
 import synth_inputs as si
@@ -15,10 +15,10 @@ class Batch:
     """Sequences of `lens` tokens of which the last `new` are rows of the batch; `lead` rows before and `tail` rows behind
     belong to nobody.  The pool holds random values in every page."""
 
-    def __init__(self, eng, lens, new, pt=64, block=1, lead=0, tail=0, seed=0, extra_pages=2, layers=1, layer=0):
+    def __init__(self, eng, lens, new, pt=64, block=1, lead=0, tail=0, seed=0, extra_pages=2, layers=1, layer=0, bits=8):
         import torch
         s, rng = eng.shape, np.random.default_rng([seed, 11])
-        self.eng, self.lens, self.layer = eng, np.asarray(lens), layer
+        self.eng, self.lens, self.layer, self.bits = eng, np.asarray(lens), layer, bits
         self.begin = lead + np.concatenate([[0], np.cumsum(new)]).astype(np.int64)
         self.rows = int(self.begin[-1]) + tail
         per = np.maximum(-(-self.lens // pt), 0)
@@ -31,7 +31,7 @@ class Batch:
             self.table[i, :n] = order[at:at + n]
             at += n
         dims = (self.n_pages, s.n_kv, pt, s.head_dim)
-        self.pages = serving.Pages(self.n_pages, s.n_kv, pt, s.head_dim, block)
+        self.pages = serving.Pages(self.n_pages, s.n_kv, pt, s.head_dim, block, bits)
         for which in (0, 1):
             self.pages.fill(rng.standard_normal(dims) * np.exp(0.5 * rng.standard_normal(dims[:3] + (1,))), which)
         self.pool = torch.zeros((layers, self.n_pages, self.pages.bytes().shape[1]), dtype=torch.uint8, device="cuda")
@@ -42,12 +42,12 @@ class Batch:
         self.q8 = self.describe()
 
     def describe(self, **kw):
-        return self.eng.q8_batch(self.pool, self.d_table, self.d_lens, self.d_begin, **dict(dict(
+        return (self.eng.q8_batch if self.bits == 8 else self.eng.q4_batch)(self.pool, self.d_table, self.d_lens, self.d_begin, **dict(dict(
             n_rows=self.rows, page_tokens=self.pt, scale_tokens=self.block, max_rows=int(self.new.max()), max_len=int(self.lens.max())), **kw))
 
     def pages_now(self):
         s = self.eng.shape
-        return serving.Pages(self.n_pages, s.n_kv, self.pt, s.head_dim, self.block).take(self.pool[self.layer].cpu().numpy())
+        return serving.Pages(self.n_pages, s.n_kv, self.pt, s.head_dim, self.block, self.bits).take(self.pool[self.layer].cpu().numpy())
 
 
 def attention_bound(kind, hd, want, size, mass, reach, most_keys):
