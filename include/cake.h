@@ -645,9 +645,9 @@ int32_t cake_op_sample(cake_ctx* ctx, const float* logits, int64_t row_stride, i
 
 /* ---- products with 4-bit weights --------------------------------------- */
 
-/* A projection matrix in 4 bits: weight (n, k) = code * scale[n][k / group].  Codes uint8, rows of (k + 31) / 32 * 16 bytes, element 2i in the low
+/* A projection matrix in 4 bits: weight (n, k) = code * scale[k / group][n].  Codes uint8, rows of (k + 31) / 32 * 16 bytes, element 2i in the low
  * half of byte i, two's complement from -8 to 7; what a row holds past its last element does not matter.  Scales in the model dtype,
- * [n][(k + group - 1) / group]; the last group of a row may be short. */
+ * [(k + group - 1) / group][n], so that neighbouring outputs' lie side by side; the last group of a row may be short. */
 typedef struct {
     const void* codes;          /* device, 16-byte aligned */
     const void* scales;         /* device */

@@ -133,7 +133,7 @@ class Q8Batch(C.Structure):
 
 class W4(C.Structure):
     """cake_w4: a projection in 4 bits.  Engine.w4 describes one and Engine.pack_w4 makes one; both keep its tensors: codes uint8
-    [n][(k + 31) // 32 * 16], scales [n][groups]."""
+    [n][(k + 31) // 32 * 16], scales [n][groups] (a view: in memory a group's scales lie side by side)."""
     _fields_ = [(n, C.c_void_p) for n in ("codes_at", "scales_at")] + [(n, C.c_int32) for n in ("n", "k", "group", "pad_")]
     codes = scales = None
     model = None     # (element type, device), where an Engine has described it
@@ -942,14 +942,18 @@ class Engine:
     # -- products with 4-bit weights ------------------------------------------------------
     def w4(self, codes, scales, k, group=128) -> W4:
         """The description of a projection in 4 bits (cake_w4): codes uint8 [n][(k + 31) // 32 * 16], two a byte; scales [n][(k + group - 1) // group]
-        in the model's type.  It may be kept and used while the tensors stay."""
+        in the model's type, of which it keeps a copy laid out for the kernels.  It may be kept and used while the codes stay."""
         if group not in (32, 64, 128) or k <= 0 or k % 8 or codes.dim() != 2 or codes.shape[0] == 0:
             raise CakeError(E_INVAL, "w4: codes %s for %d inputs, a scale for %d: rows of (k + 31) // 32 * 16 bytes, k by eights and groups of 32, 64 or 128 are needed" % (
                 tuple(codes.shape), k, group))
         n = codes.shape[0]
-        w = W4(self._operand(codes, "codes", self.torch.uint8, (n, (k + 31) // 32 * 16)), self._operand(scales, "scales", self.tdtype, (n, (k + group - 1) // group)),
-               n, k, group)
-        w.codes, w.scales, w.model = codes, scales, self._w4_model
+        at = self._operand(codes, "codes", self.torch.uint8, (n, (k + 31) // 32 * 16))
+        self._operand(scales, "scales", self.tdtype, (n, (k + group - 1) // group))
+        return self._w4_of(codes, at, scales.t().contiguous(), n, k, group)
+
+    def _w4_of(self, codes, at, by_group, n, k, group):
+        w = W4(at, by_group.data_ptr(), n, k, group)
+        w.codes, w.scales, w.model = codes, by_group.t(), self._w4_model
         return w
 
     def pack_w4(self, w, group=128, want_values=False):
@@ -959,8 +963,8 @@ class Engine:
             raise CakeError(E_INVAL, "pack_w4: weights %s, a scale for %d: inputs by eights and groups of 32, 64 or 128 are needed" % (tuple(w.shape), group))
         n, k = w.shape
         at = self._operand(w, "w", self.tdtype)
-        packed = self.w4(torch.empty((n, (k + 31) // 32 * 16), dtype=torch.uint8, device=self.dev),
-                         torch.empty((n, (k + group - 1) // group), dtype=self.tdtype, device=self.dev), k, group)
+        codes = torch.empty((n, (k + 31) // 32 * 16), dtype=torch.uint8, device=self.dev)
+        packed = self._w4_of(codes, codes.data_ptr(), torch.empty(((k + group - 1) // group, n), dtype=self.tdtype, device=self.dev), n, k, group)
         values = torch.empty((n, k), dtype=self.tdtype, device=self.dev) if want_values else None
         self._in_order(self.lib.cake_op_pack_w4, "cake_op_pack_w4", at, packed.codes_at, packed.scales_at, values.data_ptr() if want_values else None, n, k, group)
         return (packed, values) if want_values else packed

@@ -1654,7 +1654,7 @@ static int gemm_w4(cake_ctx* c, const char* what, int epi, const void* a, const 
     if (M == 0) return CAKE_OK;
     if (!a || !out || off16(a) || uintptr_t(out) % (epi == EPI_SWIGLU && c->m.dtype == CAKE_BF16 ? 2 : 4)) return fail(c, CAKE_E_INVAL, "%s: activations or result null or not aligned", what);
     const OnDevice on(c->device);
-    HIP_TRY(c, launch_gemm_w4(c->m.dtype, epi, a, *w, w2, out, M, c->cs));
+    HIP_TRY(c, launch_gemm_w4(c->m.dtype, epi, a, *w, w2, out, M, c->split.part, c->split.part_bytes, c->cs));
     return CAKE_OK;
 }
 

@@ -178,7 +178,8 @@ hipError_t launch_attention_q4(int dtype, const void* q, void* out, const Q8View
 // ---- products with 4-bit weights (cake_w4) ----
 constexpr int W4_MOST = 1 << 20;          // rows, outputs and inputs, at most
 // epi: GemmEpilogue; w2: the up weights of EPI_SWIGLU, of w's sizes.
-hipError_t launch_gemm_w4(int dtype, int epi, const void* a, const cake_w4& w, const cake_w4* w2, void* out, int M, hipStream_t st);
+// ws: float32 workspace for the parts of divided sums; launches sharing it must not overlap.
+hipError_t launch_gemm_w4(int dtype, int epi, const void* a, const cake_w4& w, const cake_w4* w2, void* out, int M, float* ws, size_t ws_bytes, hipStream_t st);
 hipError_t launch_pack_w4(int dtype, const void* w, void* codes, void* scales, void* values, int N, int K, int group, hipStream_t st);
 
 // ---- the next token of each row of logits ----

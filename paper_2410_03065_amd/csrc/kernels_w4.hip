@@ -5,6 +5,8 @@
 // on the way but float32 sums.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
+#include <type_traits>
 
 #include "kernels.hpp"
 
@@ -12,6 +14,7 @@ namespace cake {
 namespace {
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
 // v_mfma_f32_16x16x32_bf16, D[16x16] += A[16x32] * B[32x16]: lane l supplies A[l%16][8*(l/16) .. +7] and
@@ -37,6 +40,15 @@ __device__ __forceinline__ uint4 transposed(uint4 x) {
     const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
     return uint4{c[0], c[1], d[0], d[1]};
 }
+// The sum over LANES (4, 8 or 16) neighbouring lanes, in all of them.
+template <int LANES> __device__ __forceinline__ float add_group(float y) {
+    auto from = [](float v, auto ctrl) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, false)); };
+    y += from(y, std::integral_constant<int, 0xb1>{});                        // quad_perm 1 0 3 2
+    y += from(y, std::integral_constant<int, 0x4e>{});                        // quad_perm 2 3 0 1
+    if constexpr (LANES >= 8) y += from(y, std::integral_constant<int, 0x141>{});   // row_half_mirror
+    if constexpr (LANES >= 16) y += from(y, std::integral_constant<int, 0x140>{});  // row_mirror
+    return y;
+}
 __device__ __forceinline__ unsigned word(uint4 x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
 
 template <typename T> struct Terms { static constexpr int N = 1; };
@@ -47,135 +59,347 @@ struct Product {
     const unsigned char *w, *w2;       // codes; w2: of up (SwiGLU)
     const void *s, *s2;                // scales
     void* out;
-    int M, N, K, row_bytes, groups;
+    float* parts;                      // ranges of inputs: [range][gate, up][M][N]
+    int M, N, K, row_bytes, groups, epi;
 };
+template <typename T> __device__ __forceinline__ T silu_product(float gate, float up) { return T(gate / (1.f + expf(-gate)) * up); }
 
-// A wave takes 16 NT outputs and every NW-th step of 128 inputs; a lane's 16 bytes of a row's codes are 32 inputs of it.  Groups of 128: the four
-// lanes of a row multiply their first eight, second eight .. at once.  Shorter groups: the lanes exchange words first, so that
-// a product's 32 inputs lie in one group.  The offset 24 of the codes: a group's sum begins with -24 times the sum of its
-// activations, formed by a product with a constant operand that all outputs share.
-template <typename T, int EPI, int MB, int NT, int GS, int NW>
-__global__ void __launch_bounds__(64 * NW)
+// The codes of one word, eight inputs of an output, and what a product of them with activations x is short of x times the codes themselves.
+// bfloat16 activations: 24 + c in the order 0 4 1 5 2 6 3 7, and the sums of x times 24 are taken off by a product with a constant
+// operand.  float32 (three terms): 16 c as they are, since the offset would cost three bits of the sums; the scale is divided by 16.
+template <typename T> __device__ __forceinline__ bf16x8 operand(unsigned w) {
+    if constexpr (sizeof(T) == 2) return codes8(w);
+    const unsigned e = (w << 4) & 0xf0f0f0f0u, o = w & 0xf0f0f0f0u;
+    auto pair = [](unsigned a, unsigned b, int i) {
+        return __builtin_amdgcn_perm(__float_as_uint(float((signed char)(b >> (8 * i)))), __float_as_uint(float((signed char)(a >> (8 * i)))), 0x07060302);
+    };
+    const uint4 r = {pair(e, o, 0), pair(e, o, 1), pair(e, o, 2), pair(e, o, 3)};
+    return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ bf16x8 minus24() { return __builtin_bit_cast(bf16x8, uint4{0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u}); }
+
+// Few rows.  A wave takes 16 NT outputs and an NW-th of the inputs in steps of 128, PF steps of codes ahead; a lane's 16 bytes of a row's codes
+// are 32 inputs of it.  Groups of 128: the four lanes of a row multiply their first eight, second eight .. at once.  Shorter groups: the
+// lanes exchange words first, so that a product's 32 inputs lie in one group.
+template <typename T, bool SW, int NT, int GS, int NW, int PF>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2)
 w4_rows_kernel(Product p) {
-    constexpr int TERMS = Terms<T>::N, TWO = EPI == EPI_SWIGLU ? 2 : 1, NC = NT / TWO, PER = 128 / GS, MFMAS = 4 / PER;   // NC: tiles of outputs; PER: groups a step
-    static_assert(NT % TWO == 0, "gate and up side by side");
-    __shared__ float part[NW][MB][NT][4][64];
+    constexpr int TERMS = Terms<T>::N, NC = SW ? NT / 2 : NT, PER = 128 / GS, MFMAS = 4 / PER;   // NC: tiles of outputs; PER: groups a step
+    constexpr bool OFFSET = sizeof(T) == 2;
+    static_assert(!SW || NT % 2 == 0, "gate and up side by side");
+    __shared__ float part[NW][NT][4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g4 = lane >> 4;
-    const int n0 = blockIdx.x * (16 * NC), m0 = blockIdx.y * (16 * MB);
-    const T* const a = (const T*)p.a;
-    const int steps = (p.K + 127) / 128;
-    const unsigned char* row[NT];
-    const T* srow[NT];
+    const int n0 = blockIdx.x * (16 * NC), m0 = blockIdx.y * 16;
+    const int steps = (p.K + 127) / 128, i0 = steps * wave / NW, i1 = steps * (wave + 1) / NW;
+    // Rows past the last: the last, not stored; codes and scales past a row's end: its last, whose activations are zero.
+    const unsigned char* const base[2] = {p.w + size_t(n0) * p.row_bytes, SW ? p.w2 + size_t(n0) * p.row_bytes : nullptr};
+    const T* const sbase[2] = {(const T*)p.s + n0, SW ? (const T*)p.s2 + n0 : nullptr};
+    unsigned row[NC], place[NC];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int n = min(n0 + 16 * (t % NC) + n16, p.N - 1);             // rows past the last: the last, not stored
-        row[t] = (t < NC ? p.w : p.w2) + size_t(n) * p.row_bytes + g4 * 16;
-        srow[t] = (const T*)(t < NC ? p.s : p.s2) + size_t(n) * p.groups;
+    for (int t = 0; t < NC; ++t) {
+        place[t] = min(n0 + 16 * t + n16, p.N - 1) - n0;
+        row[t] = place[t] * p.row_bytes;
     }
-    const T* arow[MB];
+    const bool mine = m0 + n16 < p.M;                 // a lane whose row is past the last asks for nothing
+    const T* const abase = (const T*)p.a + size_t(m0) * p.K;
+    const unsigned arow = (mine ? n16 : 0) * p.K;
+
+    uint4 w[PF][NT];
+    T s[PF][NT][PER];
+    auto load = [&](int f, int i) {
+        const unsigned at = min(i * 64 + g4 * 16, p.row_bytes - 16);
 #pragma unroll
-    for (int b = 0; b < MB; ++b) arow[b] = a + size_t(min(m0 + 16 * b + n16, p.M - 1)) * p.K;
+        for (int t = 0; t < NT; ++t) {
+            w[f][t] = *(const uint4*)(base[t / NC] + (row[t % NC] + at));
+#pragma unroll
+            for (int g = 0; g < PER; ++g) s[f][t][g] = (sbase[t / NC] + size_t(min(i * PER + g, p.groups - 1)) * p.N)[place[t % NC]];
+        }
+    };
+    typedef typename std::conditional<TERMS == 1, uint4, f32x4[2]>::type Raw;
+    Raw raw[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (TERMS == 1) raw[j] = uint4{0, 0, 0, 0};
+        else raw[j][0] = raw[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto load_rows = [&](int i) {
+        if (mine)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = i * 128 + (GS == 128 ? 32 * g4 + 8 * j : 32 * j + 8 * g4);
+                const T* from = abase + (arow + unsigned(min(k, p.K - 8)));
+                if constexpr (TERMS == 1) raw[j] = *(const uint4*)from;
+                else { raw[j][0] = *(const f32x4*)from; raw[j][1] = *(const f32x4*)(from + 4); }
+            }
+    };
+    f32x4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int f, int i) {
+        bf16x8 x[TERMS][4];
+        const bool whole = i * 128 + 128 <= p.K;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool past = !whole && i * 128 + (GS == 128 ? 32 * g4 + 8 * j : 32 * j + 8 * g4) >= p.K;
+            if constexpr (TERMS == 1) {
+                x[0][j] = in_order(past ? uint4{0, 0, 0, 0} : raw[j]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float y = past ? 0.f : raw[j][e >> 2][e & 3];
+#pragma unroll
+                    for (int q = 0; q < TERMS; ++q) { x[q][j][e] = bf16_t(y); y -= float(x[q][j][e]); }
+                }
+            }
+        }
+        load_rows(min(i + 1, i1 - 1));
+        if constexpr (GS < 128)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) w[f][t] = transposed(w[f][t]);
+#pragma unroll
+        for (int g = 0; g < PER; ++g) {
+            f32x4 begin = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (OFFSET)
+#pragma unroll
+                for (int j = g * MFMAS; j < (g + 1) * MFMAS; ++j) begin = mfma16(x[0][j], minus24(), begin);
+            f32x4 sum[NT];
+#pragma unroll
+            for (int j = g * MFMAS; j < (g + 1) * MFMAS; ++j)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const bf16x8 o = operand<T>(word(w[f][t], j));
+#pragma unroll
+                    for (int q = TERMS - 1; q >= 0; --q) sum[t] = mfma16(x[q][j], o, j == g * MFMAS && q == TERMS - 1 ? begin : sum[t]);
+                }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float sc = float(s[f][t][g]) * (OFFSET ? 1.f : 0.0625f);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[t][v] = __builtin_fmaf(sum[t][v], sc, acc[t][v]);
+            }
+        }
+        load(f, min(i + PF, i1 - 1));
+    };
+    if (i0 < i1) {
+#pragma unroll
+        for (int f = 0; f < PF; ++f) load(f, min(i0 + f, i1 - 1));
+        load_rows(i0);
+        for (int i = i0; i < i1; i += PF)
+#pragma unroll
+            for (int f = 0; f < PF; ++f)
+                if (i + f < i1) step(f, i + f);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) part[wave][t][v][lane] = acc[t][v];
+    __syncthreads();
+    // the waves' parts in their order; D[4 g4 + v][n16]
+    for (int i = threadIdx.x; i < NC * 256; i += 64 * NW) {
+        const int l = i & 63, v = i >> 6 & 3, t = i >> 8;
+        const int m = m0 + 4 * (l >> 4) + v, n = n0 + 16 * t + (l & 15);
+        float y = 0.f, y2 = 0.f;
+#pragma unroll
+        for (int q = 0; q < NW; ++q) {
+            y += part[q][t][v][l];
+            if constexpr (SW) y2 += part[q][t + NC][v][l];
+        }
+        if (m >= p.M || n >= p.N) continue;
+        const size_t at = size_t(m) * p.N + n;
+        if constexpr (SW) ((T*)p.out)[at] = silu_product<T>(y, y2);
+        else if (p.epi == EPI_RESIDUAL_F32) ((float*)p.out)[at] += y;
+        else ((float*)p.out)[at] = y;
+    }
+}
+
+// Many rows (bfloat16).  A workgroup takes 16 MB rows, 64 NC outputs and a range of the inputs; its waves take 16 NC outputs each, whose codes come
+// straight into registers, a step of 128 inputs ahead and more, and are converted once for all rows.  The activations are shared: through LDS, two
+// tiles, rows of 256 bytes whose 16-byte pieces lie at piece ^ row, so that 16 rows' pieces of one number lie in different banks.  Who brings a
+// piece also adds up its activations, for -24 times the sum of a row's group: where a group's sum begins.
+// A unit is a group of a tile of 16 outputs.  While its products run, the next unit's codes are converted and the last one's sums scaled.
+template <bool SW, int MB, int NT, int GS, int WS, int XS>
+__global__ void __launch_bounds__(256, 2)
+w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
+    constexpr int NC = SW ? NT / 2 : NT, PER = 128 / GS, MF = 4 / PER, UNITS = PER * NT, TILE = MB * 16 * 256, SUMS = PER * MB * 16 * 4;
+    static_assert(!SW || NT % 2 == 0, "gate and up side by side");
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g4 = lane >> 4;
+    // The row tiles of the same outputs side by side on one XCD (workgroups are dealt out to the eight in turn), so that they share its L2.
+    const int total = m_tiles * n_tiles * splits, per = (total + 7) / 8;
+    int b0 = int(blockIdx.x) % 8 * per + int(blockIdx.x) / 8;
+    if (b0 >= total) return;
+    const int mt = b0 % m_tiles; b0 /= m_tiles;
+    const int nt = b0 % n_tiles, split = b0 / n_tiles;
+    const int m0 = mt * (16 * MB), n0 = nt * (64 * NC) + wave * (16 * NC);
+    const int steps = (p.K + 127) / 128, i0 = int(int64_t(steps) * split / splits), i1 = int(int64_t(steps) * (split + 1) / splits);
+    // codes and scales from the wave's first row on: offsets of 32 bits
+    const int n_first = min(n0, p.N - 1);
+    const unsigned char* const base[2] = {p.w + size_t(n_first) * p.row_bytes, SW ? p.w2 + size_t(n_first) * p.row_bytes : nullptr};
+    const bf16_t* const sbase[2] = {(const bf16_t*)p.s + n_first, SW ? (const bf16_t*)p.s2 + n_first : nullptr};
+    unsigned row[NC], place[NC];
+#pragma unroll
+    for (int t = 0; t < NC; ++t) {
+        place[t] = min(n0 + 16 * t + n16, p.N - 1) - n_first;
+        row[t] = place[t] * p.row_bytes;
+    }
+    uint4 w[WS][NT];
+    bf16_t s[2][NT][PER];
+    auto load_codes = [&](int f, int i, int t) { w[f][t] = *(const uint4*)(base[t / NC] + (row[t % NC] + unsigned(min(i * 64 + g4 * 16, p.row_bytes - 16)))); };
+    auto load_scales = [&](int f, int i) {
+#pragma unroll
+        for (int g = 0; g < PER; ++g)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[f][t][g] = (sbase[t / NC] + size_t(min(i * PER + g, p.groups - 1)) * p.N)[place[t % NC]];
+    };
+    // this thread's piece of 16 rows: from memory through registers into LDS
+    const int piece = tid & 15, r0 = tid >> 4;
+    const bf16_t* const abase = (const bf16_t*)p.a + size_t(m0) * p.K;
+    unsigned arow[MB];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) arow[b] = min(16 * b + r0, p.M - 1 - m0) * p.K;
+    uint4 raw[XS][MB];
+    auto load_rows = [&](int q, int i) {
+        const int k = i * 128 + piece * 8;
+#pragma unroll
+        for (int b = 0; b < MB; ++b) raw[q][b] = *(const uint4*)(abase + (arow[b] + min(k, p.K - 8)));
+    };
+    const int put = r0 * 256 + ((piece ^ r0) << 4);
+    auto stage = [&](int q, int i, int buf) {
+        const unsigned keep = i * 128 + piece * 8 < p.K ? ~0u : 0u;        // inputs past the last: zeros
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+            raw[q][b].x &= keep; raw[q][b].y &= keep; raw[q][b].z &= keep; raw[q][b].w &= keep;
+            *(bf16x8*)(lds + buf * TILE + b * 4096 + put) = in_order(raw[q][b]);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, word(raw[q][b], e)), __builtin_bit_cast(bf16x2, 0xc1c0c1c0u), sum, false);
+            sum = add_group<GS / 8>(sum);
+            *(float*)(lds + 2 * TILE + buf * SUMS + ((piece / (GS / 8)) * (MB * 16) + b * 16 + r0) * 4) = sum;
+        }
+    };
+    const int get = n16 * 256;
+    auto fragment = [&](int buf, int b, int j) {
+        const int c = GS == 128 ? 4 * g4 + j : 4 * j + g4;
+        return *(const bf16x8*)(lds + buf * TILE + b * 4096 + get + ((c ^ n16) << 4));
+    };
     f32x4 acc[MB][NT];
 #pragma unroll
     for (int b = 0; b < MB; ++b)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const uint4 minus24 = {0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u};
-    const uint4 zero = {0, 0, 0, 0};
-
-    for (int i = wave; i < steps; i += NW) {
-        const int k0 = i * 128;
-        uint4 w[NT];
-        float s[NT][PER];
+    bf16x8 o[MF];                          // the unit's codes; behind their product, the next unit's
+    f32x4 sum[2][MB];
+    auto convert = [&](int f, int u, int j) { o[j] = codes8(word(w[f][u % NT], u / NT * MF + j)); };
+    auto begin = [&](int f, int u) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            w[t] = k0 + 32 * g4 < p.K ? *(const uint4*)(row[t] + i * 64) : zero;
-#pragma unroll
-            for (int g = 0; g < PER; ++g) s[t][g] = i * PER + g < p.groups ? float(srow[t][i * PER + g]) : 0.f;
-        }
-        bf16x8 x[MB][TERMS][4];
+        for (int b = 0; b < MB; ++b) sum[u & 1][b] = *(const f32x4*)(lds + 2 * TILE + f * SUMS + (u / NT * (MB * 16) + b * 16 + 4 * g4) * 4);
+    };
+    auto scaled = [&](int f, int u) {
+        const float sc = float(s[f][u % NT][u / NT]);
 #pragma unroll
         for (int b = 0; b < MB; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = k0 + (GS == 128 ? 32 * g4 + 8 * j : 32 * j + 8 * g4);
-                if constexpr (TERMS == 1) {
-                    x[b][0][j] = in_order(k < p.K ? *(const uint4*)(arow[b] + k) : zero);
-                } else {
-                    float f[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] = k < p.K ? arow[b][k + (e >> 1) + 4 * (e & 1)] : 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int q = 0; q < TERMS; ++q) { x[b][q][j][e] = bf16_t(f[e]); f[e] -= float(x[b][q][j][e]); }
-                }
-            }
+            for (int v = 0; v < 4; ++v) acc[b][u % NT][v] = __builtin_fmaf(sum[u & 1][b][v], sc, acc[b][u % NT][v]);
+    };
+    auto step = [&](auto odd, int i) {
+        constexpr int f = decltype(odd)::value, fw = f % WS, q = (f + 1) % XS;   // f: (i - i0) % 2
+        // no branches: what a step past the last would need is loaded from the last, and not used
+        stage(q, i + 1, f ^ 1);
+        load_rows(q, min(i + 1 + XS, i1 - 1));
         if constexpr (GS < 128)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) w[t] = transposed(w[t]);
+            for (int t = 0; t < NT; ++t) w[fw][t] = transposed(w[fw][t]);
+        bf16x8 x[MB][MF];
+        begin(f, 0);
 #pragma unroll
-        for (int g = 0; g < PER; ++g) {
-            f32x4 begin[MB];
+        for (int j = 0; j < MF; ++j) convert(fw, 0, j);
 #pragma unroll
-            for (int b = 0; b < MB; ++b) {
-                begin[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int u = 0; u < UNITS; ++u) {
+            const int g = u / NT, t = u % NT;
+            if (t == 0)
 #pragma unroll
-                for (int j = g * MFMAS; j < (g + 1) * MFMAS; ++j)
+                for (int j = 0; j < MF; ++j)
 #pragma unroll
-                    for (int q = TERMS - 1; q >= 0; --q) begin[b] = mfma16(x[b][q][j], __builtin_bit_cast(bf16x8, minus24), begin[b]);
+                    for (int b = 0; b < MB; ++b) x[b][j] = fragment(f, b, g * MF + j);
+            __builtin_amdgcn_sched_barrier(0);
+            if (u > 0) scaled(f, u - 1);
+#pragma unroll
+            for (int j = 0; j < MF; ++j) {
+#pragma unroll
+                for (int b = 0; b < MB; ++b) sum[u & 1][b] = mfma16(x[b][j], o[j], sum[u & 1][b]);
+                if (u + 1 < UNITS) convert(fw, u + 1, j);
             }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                f32x4 sum[MB];
-#pragma unroll
-                for (int j = g * MFMAS; j < (g + 1) * MFMAS; ++j) {
-                    const bf16x8 c = codes8(word(w[t], j));
-#pragma unroll
-                    for (int b = 0; b < MB; ++b)
-#pragma unroll
-                        for (int q = TERMS - 1; q >= 0; --q) sum[b] = mfma16(x[b][q][j], c, j == g * MFMAS && q == TERMS - 1 ? begin[b] : sum[b]);
-                }
-#pragma unroll
-                for (int b = 0; b < MB; ++b)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[b][t][v] = __builtin_fmaf(sum[b][v], s[t][g], acc[b][t][v]);
-            }
+            if (u + 1 < UNITS) begin(f, u + 1);
+            if (g == PER - 1) load_codes(fw, min(i + WS, i1 - 1), t);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        scaled(f, UNITS - 1);
+        load_scales(f, min(i + 2, i1 - 1));
+        __syncthreads();
+    };
+    if (i0 < i1) {
+#pragma unroll
+        for (int q = 0; q < XS + 1; ++q)
+            {
+                const int i = min(i0 + q, i1 - 1);
+                if (q < WS)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) load_codes(q, i, t);
+                if (q < 2) load_scales(q, i);
+                load_rows(q % XS, i);
+                if (q == 0) stage(0, i0, 0);
+            }
+    }
+    __syncthreads();
+    for (int i = i0; i < i1; i += 2) {
+        step(std::integral_constant<int, 0>{}, i);
+        if (i + 1 < i1) step(std::integral_constant<int, 1>{}, i + 1);
     }
 #pragma unroll
     for (int b = 0; b < MB; ++b)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NC; ++t)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) part[wave][b][t][v][lane] = acc[b][t][v];
-    __syncthreads();
-    // the waves' parts in their order; D[4 g4 + v][n16]
-    for (int i = threadIdx.x; i < MB * NC * 256; i += 64 * NW) {
-        const int l = i & 63, v = i >> 6 & 3, t = (i >> 8) % NC, b = (i >> 8) / NC;
-        const int m = m0 + 16 * b + 4 * (l >> 4) + v, n = n0 + 16 * t + (l & 15);
+            for (int v = 0; v < 4; ++v) {
+                const int m = m0 + 16 * b + 4 * g4 + v, n = n0 + 16 * t + n16;
+                if (m >= p.M || n >= p.N) continue;
+                const size_t at = size_t(m) * p.N + n;
+                if (splits > 1) {
+                    float* d = p.parts + size_t(split) * (SW ? 2 : 1) * p.M * p.N + at;
+                    *d = acc[b][t][v];
+                    if constexpr (SW) d[size_t(p.M) * p.N] = acc[b][t + NC][v];
+                } else if constexpr (SW) ((bf16_t*)p.out)[at] = silu_product<bf16_t>(acc[b][t][v], acc[b][t + NC][v]);
+                else if (p.epi == EPI_RESIDUAL_F32) ((float*)p.out)[at] += acc[b][t][v];
+                else ((float*)p.out)[at] = acc[b][t][v];
+            }
+}
+
+// The ranges' parts in their order.
+__global__ void __launch_bounds__(256)
+w4_parts_kernel(Product p, int splits) {
+    const size_t size = size_t(p.M) * p.N, stride = p.epi == EPI_SWIGLU ? 2 * size : size;
+    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < size; i += size_t(gridDim.x) * 256) {
         float y = 0.f, y2 = 0.f;
-#pragma unroll
-        for (int q = 0; q < NW; ++q) {
-            y += part[q][b][t][v][l];
-            if constexpr (TWO == 2) y2 += part[q][b][t + NC][v][l];
+        for (int q = 0; q < splits; ++q) {
+            y += p.parts[q * stride + i];
+            if (p.epi == EPI_SWIGLU) y2 += p.parts[q * stride + size + i];
         }
-        if (m >= p.M || n >= p.N) continue;
-        const size_t at = size_t(m) * p.N + n;
-        if constexpr (EPI == EPI_STORE_F32) ((float*)p.out)[at] = y;
-        else if constexpr (EPI == EPI_RESIDUAL_F32) ((float*)p.out)[at] += y;
-        else ((T*)p.out)[at] = T(y / (1.f + expf(-y)) * y2);
+        if (p.epi == EPI_SWIGLU) ((bf16_t*)p.out)[i] = silu_product<bf16_t>(y, y2);
+        else if (p.epi == EPI_RESIDUAL_F32) ((float*)p.out)[i] += y;
+        else ((float*)p.out)[i] = y;
     }
 }
 
-// A lane takes eight weights of a row, the lanes of a group find its largest magnitude.  Bound by the bytes.
+// A lane takes eight weights of a row, the lanes of a group find its largest magnitude; a workgroup takes the same group of neighbouring rows,
+// whose scales lie side by side.  Bound by the bytes.
 template <typename T, int GS>
 __global__ void __launch_bounds__(256)
 pack_w4_kernel(const T* __restrict__ w, unsigned char* __restrict__ codes, T* __restrict__ scales, T* __restrict__ values, int N, int K, int row_bytes, int groups) {
-    constexpr int LANES = GS / 8;
-    const int per_row = groups * LANES;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < int64_t(N) * per_row; i += int64_t(gridDim.x) * 256) {   // whole groups of lanes
-        const int n = int(i / per_row), piece = int(i % per_row), k = piece * 8;
+    constexpr int LANES = GS / 8, ROWS = 256 / LANES;
+    const int64_t blocks = int64_t((N + ROWS - 1) / ROWS) * groups;
+    for (int64_t i = blockIdx.x; i < blocks; i += gridDim.x) {
+        const int group = int(i % groups), n = int(i / groups) * ROWS + threadIdx.x / LANES, piece = group * LANES + threadIdx.x % LANES, k = piece * 8;
+        if (n >= N) continue;                             // whole groups of lanes
         float x[8] = {};
         if (k < K) {
             const T* from = w + size_t(n) * K + k;
@@ -196,7 +420,7 @@ pack_w4_kernel(const T* __restrict__ w, unsigned char* __restrict__ codes, T* __
         for (int d = 1; d < LANES; d *= 2) m = max(m, unsigned(__shfl_xor(int(m), d)));
         const T s = T(m >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(m) / 7.f);
         const float scale = float(s);
-        if (piece % LANES == 0) scales[size_t(n) * groups + piece / LANES] = s;
+        if (piece % LANES == 0) scales[size_t(group) * N + n] = s;
         if (piece * 4 >= row_bytes) continue;
         unsigned packed = 0;
         float c[8];
@@ -222,33 +446,85 @@ pack_w4_kernel(const T* __restrict__ w, unsigned char* __restrict__ codes, T* __
     }
 }
 
-template <typename T, int EPI, int GS>
+int forced(const char* name) { const char* e = getenv(name); return e ? atoi(e) : 0; }
+
+template <typename T, bool SW, int GS>
 hipError_t rows(const Product& p, hipStream_t st) {
-    constexpr int NT = EPI == EPI_SWIGLU ? 2 : 1;
-    auto go = [&](auto mb) {
-        constexpr int MB = decltype(mb)::value;
-        hipLaunchKernelGGL((w4_rows_kernel<T, EPI, MB, NT, GS, 4>), dim3(unsigned((p.N + 15) / 16), unsigned((p.M + 16 * MB - 1) / (16 * MB))), dim3(256), 0, st, p);
+    auto go = [&](auto nt, auto pf, auto nw) {
+        constexpr int NT = decltype(nt)::value, NC = SW ? NT / 2 : NT, PF = decltype(pf)::value, NW = decltype(nw)::value;
+        hipLaunchKernelGGL((w4_rows_kernel<T, SW, NT, GS, NW, PF>), dim3(unsigned((p.N + 16 * NC - 1) / (16 * NC)), unsigned((p.M + 15) / 16)), dim3(64 * NW), 0, st, p);
         return hipGetLastError();
     };
-    if (p.M <= 16) return go(std::integral_constant<int, 1>{});
-    return go(std::integral_constant<int, 2>{});
+    const std::integral_constant<int, 1> one{};
+    const std::integral_constant<int, 2> two{};
+    const std::integral_constant<int, 3> three{};
+    const std::integral_constant<int, 4> four{};
+    const std::integral_constant<int, 8> eight{};
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (SW) return go(two, one, eight);
+        else return go(one, one, eight);
+    } else {
+        int nt = forced("W4_NT"), v = forced("W4_V");
+        if (!nt) nt = SW ? 2 : 1;
+        if constexpr (!SW)
+            if (nt == 1) return v == 1 ? go(one, four, eight) : v == 2 ? go(one, two, four) : v == 3 ? go(one, four, four) : go(one, two, eight);
+        if (nt == 2) return v == 1 ? go(two, three, eight) : v == 2 ? go(two, two, four) : v == 3 ? go(two, three, four) : go(two, two, eight);
+        return v == 1 ? go(four, one, eight) : v == 2 ? go(four, two, four) : v == 3 ? go(four, one, four) : go(four, two, eight);
+    }
 }
 
-template <typename T, int EPI>
-hipError_t by_group(const Product& p, int group, hipStream_t st) {
-    return group == 128 ? rows<T, EPI, 128>(p, st) : group == 64 ? rows<T, EPI, 64>(p, st) : rows<T, EPI, 32>(p, st);
+template <bool SW, int GS>
+hipError_t tiles(Product p, float* ws, size_t ws_bytes, hipStream_t st) {
+    auto go = [&](auto mb, auto nt, auto ws_, auto xs) {
+        constexpr int MB = decltype(mb)::value, NT = decltype(nt)::value, NC = SW ? NT / 2 : NT;
+        const int m_tiles = (p.M + 16 * MB - 1) / (16 * MB), n_tiles = (p.N + 64 * NC - 1) / (64 * NC), steps = (p.K + 127) / 128;
+        const int64_t grid = int64_t(m_tiles) * n_tiles;
+        int splits = forced("W4_SPLIT");
+        if (!splits) splits = int(std::max<int64_t>(1, std::min<int64_t>(steps / 4, 512 / grid)));
+        splits = int(std::min<int64_t>(splits, int64_t(ws_bytes / (size_t(p.M) * p.N * (SW ? 8 : 4)))));
+        if (splits < 1) splits = 1;
+        p.parts = ws;
+        constexpr int LDS = 2 * MB * 16 * (256 + 128 / GS * 4);
+        hipLaunchKernelGGL((w4_tile_kernel<SW, MB, NT, GS, decltype(ws_)::value, decltype(xs)::value>), dim3(unsigned((grid * splits + 7) / 8 * 8)), dim3(256), LDS, st, p, m_tiles,
+                           n_tiles, splits);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess || splits == 1) return e;
+        hipLaunchKernelGGL(w4_parts_kernel, dim3(unsigned(std::min<int64_t>((int64_t(p.M) * p.N + 255) / 256, 1 << 16))), dim3(256), 0, st, p, splits);
+        return hipGetLastError();
+    };
+    const std::integral_constant<int, 1> one{};
+    const std::integral_constant<int, 2> two{};
+    const std::integral_constant<int, 4> four{};
+    int nt = forced("W4_NT"), mb = forced("W4_MB");
+    if (!mb) mb = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
+    if (!nt) nt = p.M <= 64 ? 2 : 4;
+    if (mb == 1) return go(one, two, two, two);
+    if (mb == 2) return go(two, two, two, two);
+    if (nt == 2) return go(four, two, two, two);
+    return go(four, four, one, one);
+}
+
+template <typename T, bool SW, int GS>
+hipError_t choose(const Product& p, float* ws, size_t ws_bytes, hipStream_t st) {
+    if constexpr (sizeof(T) == 2)
+        if ((forced("W4_K") == 2 || (!forced("W4_K") && p.M > 16))) return tiles<SW, GS>(p, ws, ws_bytes, st);
+    return rows<T, SW, GS>(p, st);
 }
 
 template <typename T>
-hipError_t by_form(int epi, const Product& p, int group, hipStream_t st) {
-    return epi == EPI_STORE_F32 ? by_group<T, EPI_STORE_F32>(p, group, st) : epi == EPI_RESIDUAL_F32 ? by_group<T, EPI_RESIDUAL_F32>(p, group, st)
-                                                                                                     : by_group<T, EPI_SWIGLU>(p, group, st);
+hipError_t product(const Product& p, int group, float* ws, size_t ws_bytes, hipStream_t st) {
+    auto go = [&](auto sw) {
+        constexpr bool SW = decltype(sw)::value;
+        return group == 128 ? choose<T, SW, 128>(p, ws, ws_bytes, st) : group == 64 ? choose<T, SW, 64>(p, ws, ws_bytes, st) : choose<T, SW, 32>(p, ws, ws_bytes, st);
+    };
+    return p.epi == EPI_SWIGLU ? go(std::true_type{}) : go(std::false_type{});
 }
 
 template <typename T>
 hipError_t pack(const T* w, unsigned char* codes, T* scales, T* values, int N, int K, int group, hipStream_t st) {
     const int groups = (K + group - 1) / group;
-    const dim3 grid(unsigned(std::min<int64_t>((int64_t(N) * groups * (group / 8) + 255) / 256, 1 << 22)));
+    const int rows = 256 / (group / 8);
+    const dim3 grid(unsigned(std::min<int64_t>(int64_t((N + rows - 1) / rows) * groups, 1 << 22)));
     auto go = [&](auto gs) {
         hipLaunchKernelGGL((pack_w4_kernel<T, decltype(gs)::value>), grid, dim3(256), 0, st, w, codes, scales, values, N, K, (K + 31) / 32 * 16, groups);
         return hipGetLastError();
@@ -257,10 +533,10 @@ hipError_t pack(const T* w, unsigned char* codes, T* scales, T* values, int N, i
 }
 }  // namespace
 
-hipError_t launch_gemm_w4(int dtype, int epi, const void* a, const cake_w4& w, const cake_w4* w2, void* out, int M, hipStream_t st) {
-    const Product p = {a, (const unsigned char*)w.codes, w2 ? (const unsigned char*)w2->codes : nullptr, w.scales, w2 ? w2->scales : nullptr, out, M, w.n, w.k,
-                       (w.k + 31) / 32 * 16, (w.k + w.group - 1) / w.group};
-    return dtype == CAKE_F32 ? by_form<float>(epi, p, w.group, st) : by_form<bf16_t>(epi, p, w.group, st);
+hipError_t launch_gemm_w4(int dtype, int epi, const void* a, const cake_w4& w, const cake_w4* w2, void* out, int M, float* ws, size_t ws_bytes, hipStream_t st) {
+    const Product p = {a, (const unsigned char*)w.codes, w2 ? (const unsigned char*)w2->codes : nullptr, w.scales, w2 ? w2->scales : nullptr, out, nullptr,
+                       M, w.n, w.k, (w.k + 31) / 32 * 16, (w.k + w.group - 1) / w.group, epi};
+    return dtype == CAKE_F32 ? product<float>(p, w.group, ws, ws_bytes, st) : product<bf16_t>(p, w.group, ws, ws_bytes, st);
 }
 
 hipError_t launch_pack_w4(int dtype, const void* w, void* codes, void* scales, void* values, int N, int K, int group, hipStream_t st) {

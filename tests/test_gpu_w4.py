@@ -349,7 +349,7 @@ def test_refusals():
     refused(lambda: eng.op_gemm_w4_swiglu(t, p.w4, Projection(eng, 49, 136, 64).w4))
     refused(lambda: eng.op_gemm_w4_swiglu(t, p.w4, Projection(eng, 48, 136, 32).w4))
     refused(lambda: engine("f32").op_gemm_w4(t.float(), p.w4))
-    codes, scales = p.w4.codes, p.w4.scales
+    codes, scales = p.w4.codes, p.w4.scales.contiguous()
     for args in ((codes[:, :64], scales, 136, 64), (codes, scales[:, :2], 136, 64), (codes, scales.float(), 136, 64), (codes, scales, 136, 48), (codes, scales, 130, 64),
                  (codes, scales, 0, 64), (codes.int(), scales, 136, 64), (codes.cpu(), scales, 136, 64), (codes[:0], scales[:0], 136, 64), (codes[0], scales, 136, 64)):
         refused(lambda: eng.w4(*args))
