@@ -218,19 +218,13 @@ w4_rows_kernel(Product p) {
 // piece also adds up its activations, for -24 times the sum of a row's group: where a group's sum begins.
 // A unit is a group of a tile of 16 outputs.  While its products run, the next unit's codes are converted and the last one's sums scaled.
 template <bool SW, int MB, int NT, int GS, int WS, int XS>
-__global__ void __launch_bounds__(256, 2)
-w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
+__device__ __forceinline__ void w4_tile(const Product& p, unsigned char* lds, int mt, int n_begin, int split, int splits) {
     constexpr int NC = SW ? NT / 2 : NT, PER = 128 / GS, MF = 4 / PER, UNITS = PER * NT, TILE = MB * 16 * 256, SUMS = PER * MB * 16 * 4;
+    constexpr int SS = WS < 2 ? 2 : WS, TURNS = WS > 2 ? WS : 2;      // sets of scales; steps until the sets come round
+    static_assert(TURNS % 2 == 0 && TURNS % XS == 0, "a step's sets are known when it is compiled");
     static_assert(!SW || NT % 2 == 0, "gate and up side by side");
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g4 = lane >> 4;
-    // The row tiles of the same outputs side by side on one XCD (workgroups are dealt out to the eight in turn), so that they share its L2.
-    const int total = m_tiles * n_tiles * splits, per = (total + 7) / 8;
-    int b0 = int(blockIdx.x) % 8 * per + int(blockIdx.x) / 8;
-    if (b0 >= total) return;
-    const int mt = b0 % m_tiles; b0 /= m_tiles;
-    const int nt = b0 % n_tiles, split = b0 / n_tiles;
-    const int m0 = mt * (16 * MB), n0 = nt * (64 * NC) + wave * (16 * NC);
+    const int m0 = mt * (16 * MB), n0 = n_begin + wave * (16 * NC);
     const int steps = (p.K + 127) / 128, i0 = int(int64_t(steps) * split / splits), i1 = int(int64_t(steps) * (split + 1) / splits);
     // codes and scales from the wave's first row on: offsets of 32 bits
     const int n_first = min(n0, p.N - 1);
@@ -243,7 +237,7 @@ w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
         row[t] = place[t] * p.row_bytes;
     }
     uint4 w[WS][NT];
-    bf16_t s[2][NT][PER];
+    bf16_t s[SS][NT][PER];
     auto load_codes = [&](int f, int i, int t) { w[f][t] = *(const uint4*)(base[t / NC] + (row[t % NC] + unsigned(min(i * 64 + g4 * 16, p.row_bytes - 16)))); };
     auto load_scales = [&](int f, int i) {
 #pragma unroll
@@ -302,7 +296,7 @@ w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
             for (int v = 0; v < 4; ++v) acc[b][u % NT][v] = __builtin_fmaf(sum[u & 1][b][v], sc, acc[b][u % NT][v]);
     };
     auto step = [&](auto odd, int i) {
-        constexpr int f = decltype(odd)::value, fw = f % WS, q = (f + 1) % XS;   // f: (i - i0) % 2
+        constexpr int turn = decltype(odd)::value, f = turn % 2, fw = turn % WS, fs = turn % SS, q = (turn + 1) % XS;   // turn: (i - i0) % TURNS
         // no branches: what a step past the last would need is loaded from the last, and not used
         stage(q, i + 1, f ^ 1);
         load_rows(q, min(i + 1 + XS, i1 - 1));
@@ -322,7 +316,7 @@ w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
 #pragma unroll
                     for (int b = 0; b < MB; ++b) x[b][j] = fragment(f, b, g * MF + j);
             __builtin_amdgcn_sched_barrier(0);
-            if (u > 0) scaled(f, u - 1);
+            if (u > 0) scaled(fs, u - 1);
 #pragma unroll
             for (int j = 0; j < MF; ++j) {
 #pragma unroll
@@ -333,27 +327,30 @@ w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
             if (g == PER - 1) load_codes(fw, min(i + WS, i1 - 1), t);
             __builtin_amdgcn_sched_barrier(0);
         }
-        scaled(f, UNITS - 1);
-        load_scales(f, min(i + 2, i1 - 1));
+        scaled(fs, UNITS - 1);
+        load_scales(fs, min(i + SS, i1 - 1));
         __syncthreads();
     };
     if (i0 < i1) {
 #pragma unroll
-        for (int q = 0; q < XS + 1; ++q)
-            {
-                const int i = min(i0 + q, i1 - 1);
-                if (q < WS)
+        for (int q = 0; q < (SS > XS + 1 ? SS : XS + 1); ++q) {
+            const int i = min(i0 + q, i1 - 1);
+            if (q < WS)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) load_codes(q, i, t);
-                if (q < 2) load_scales(q, i);
-                load_rows(q % XS, i);
-                if (q == 0) stage(0, i0, 0);
-            }
+                for (int t = 0; t < NT; ++t) load_codes(q, i, t);
+            if (q < SS) load_scales(q, i);
+            if (q <= XS) load_rows(q % XS, i);
+            if (q == 0) stage(0, i0, 0);
+        }
     }
     __syncthreads();
-    for (int i = i0; i < i1; i += 2) {
+    for (int i = i0; i < i1; i += TURNS) {
         step(std::integral_constant<int, 0>{}, i);
         if (i + 1 < i1) step(std::integral_constant<int, 1>{}, i + 1);
+        if constexpr (TURNS == 4) {
+            if (i + 2 < i1) step(std::integral_constant<int, 2>{}, i + 2);
+            if (i + 3 < i1) step(std::integral_constant<int, 3>{}, i + 3);
+        }
     }
 #pragma unroll
     for (int b = 0; b < MB; ++b)
@@ -374,17 +371,288 @@ w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
             }
 }
 
+// Workgroups are dealt out to the eight XCDs in turn.  A column (the row tiles of the same outputs and inputs) stays on one, so that they share its
+// L2; neighbouring columns go to different ones.
+struct Place { int column, mt; };
+__device__ __forceinline__ Place place_of(int b, int m_tiles) {
+    const int slot = b / 8;
+    return {slot / m_tiles * 8 + b % 8, slot % m_tiles};
+}
+inline int blocks_of(int columns, int m_tiles) { return (columns + 7) / 8 * 8 * m_tiles; }
+
+template <bool SW, int MB, int NT, int GS, int WS, int XS>
+__global__ void __launch_bounds__(256, 2)
+w4_tile_kernel(Product p, int m_tiles, int n_tiles, int splits) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const Place at = place_of(blockIdx.x, m_tiles);
+    if (at.column < n_tiles * splits) w4_tile<SW, MB, NT, GS, WS, XS>(p, lds, at.mt, at.column % n_tiles * (64 * (SW ? NT / 2 : NT)), at.column / n_tiles, splits);
+}
+
+// ---- many rows
+// The weights enter as code times scale in half precision: eleven bits, exact.  For that an output's scales are taken in units of 2^E, the
+// largest of them in [2^10, 2^11), and a row's activations in units that put the largest in [2^14, 2^15); both are exact down to 2^-24 of a
+// unit, 2^-35 of the largest scale, 2^-39 of the largest activation.  A pass before the product finds the units, and lays the activations
+// out as the product brings them into LDS: [64 inputs][row][eight pieces of eight], the pieces in the order in which a product's lanes take them, swizzled.
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+__device__ __forceinline__ f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+struct Wide {
+    Product p;
+    _Float16* x;            // [2 steps][m_pad][64]
+    float* row_unit;        // [m_pad]
+    float* out_unit;        // [2][N]: 2^(E - 10)
+    int m_pad, shift;       // 2^shift inputs share a scale
+};
+__device__ __forceinline__ float power(int biased) { return __uint_as_float(unsigned(biased) << 23); }
+
+// Workgroups for 64 outputs each, then for a row each, which is kept in registers between its largest magnitude and its place (up to 16384 inputs).
+__global__ void __launch_bounds__(256)
+w4_prepare_kernel(Wide q) {
+    constexpr int HELD = 8;
+    __shared__ unsigned top[256];
+    const Product& p = q.p;
+    const int tid = threadIdx.x, per = (p.N + 63) / 64, of_outputs = (p.s2 ? 2 : 1) * per;
+    unsigned most = 0;                                          // as bits: magnitudes order like the numbers; infinities and NaN do not count
+    if (int(blockIdx.x) < of_outputs) {
+        const int which = blockIdx.x / per, n = int(blockIdx.x) % per * 64 + (tid & 63);
+        const unsigned short* const s = (const unsigned short*)(which ? p.s2 : p.s) + min(n, p.N - 1);
+#pragma unroll 16
+        for (int g = tid >> 6; g < p.groups; g += 4) {
+            const unsigned v = s[size_t(g) * p.N] & 0x7fffu;
+            most = max(most, v < 0x7f80u ? v : 0u);
+        }
+        top[tid] = most;
+        __syncthreads();
+        if (tid < 64 && n < p.N) q.out_unit[which * p.N + n] = power(max(int(max(max(most, top[tid + 64]), max(top[tid + 128], top[tid + 192])) >> 7), 11) - 10);
+        return;
+    }
+    const int m = int(blockIdx.x) - of_outputs, chunks = (p.K + 127) / 128 * 16;
+    const bf16_t* const row = (const bf16_t*)p.a + size_t(min(m, p.M - 1)) * p.K;
+    auto read = [&](int c) { return 8 * c < p.K && m < p.M ? *(const uint4*)(row + 8 * c) : uint4{0, 0, 0, 0}; };
+    auto largest = [&](uint4 v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned lo = word(v, e) & 0x7fffu, hi = word(v, e) >> 16 & 0x7fffu;
+            most = max(most, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+        }
+    };
+    uint4 held[HELD];
+#pragma unroll
+    for (int r = 0; r < HELD; ++r) held[r] = read(tid + 256 * r);
+#pragma unroll
+    for (int r = 0; r < HELD; ++r) largest(held[r]);
+    for (int c = tid + 256 * HELD; c < chunks; c += 256) largest(read(c));
+#pragma unroll
+    for (int d = 32; d; d >>= 1) most = max(most, unsigned(__shfl_xor(int(most), d)));
+    if ((tid & 63) == 0) top[tid >> 6] = most;
+    __syncthreads();
+    const int e = max(int(max(max(top[0], top[1]), max(top[2], top[3])) >> 7), 15);
+    const float f = power(268 - e);                             // 2^(14 - (e - 127))
+    if (tid == 0) q.row_unit[m] = power(e - 14);
+    auto put = [&](int c, uint4 v) {
+        const int k = 8 * c, r = k & 127, slot = ((r >> 3 & 1) * 4 + (r >> 5)) ^ (m >> 1 & 7);
+        f16x8 h;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                           // elements i and i + 4
+            const unsigned a = word(v, i >> 1), b = word(v, 2 + (i >> 1));
+            h[2 * i] = _Float16(__uint_as_float(i & 1 ? a & 0xffff0000u : a << 16) * f);
+            h[2 * i + 1] = _Float16(__uint_as_float(i & 1 ? b & 0xffff0000u : b << 16) * f);
+        }
+        *(f16x8*)(q.x + (size_t((k >> 7) * 2 + (r >> 4 & 1)) * q.m_pad + m) * 64 + slot * 8) = h;
+    };
+#pragma unroll
+    for (int r = 0; r < HELD; ++r)
+        if (tid + 256 * r < chunks) put(tid + 256 * r, held[r]);
+    for (int c = tid + 256 * HELD; c < chunks; c += 256) put(c, read(c));
+}
+
+// Eight codes of a word times a scale: 16 + the code's four bits (the upper one turned) is 24 + c, and one multiply-add makes (24 + c) s - 24 s of it, exact.
+// s: the scale and -24 times it.
+__device__ __forceinline__ f16x8 weights8(unsigned w, f16x2 s) {
+    constexpr unsigned M = 0x03c003c0u, B = 0x4e004e00u;
+    auto pair = [&](unsigned y) { return __builtin_bit_cast(unsigned, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (y & M) ^ B), f16x2{s[0], s[0]}, f16x2{s[1], s[1]})); };
+    const uint4 r = {pair(w << 6), pair(w << 2), pair(w >> 2), pair(w >> 6)};
+    return __builtin_bit_cast(f16x8, r);
+}
+
+// A workgroup takes 16 MB rows and 64 NC outputs (SwiGLU: of each matrix), a wave all of the rows and 16 NC outputs.  Activations come into LDS in
+// halves of a step, a ring of four, by loads that pass no register; codes into registers, a step ahead.  Half-way through a half step all its
+// operands are read: there the waves meet, the next half must have come, and the third from here is asked for, into the place of the last.
+#define CAKE_LDS_AS __attribute__((address_space(3)))
+template <bool SW, int MB, int NT>
+__device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, int mt, int n_begin, int split, int splits) {
+    constexpr int NC = SW ? NT / 2 : NT, STAGE = MB * 2048, DMA = MB / 2, WS = MB < 8 ? 4 : 2;   // WS: steps of codes on their way
+    static_assert(!SW || NT % 2 == 0, "gate and up side by side");
+    static_assert(MB % 2 == 0, "a stage in whole loads of each wave");
+    const Product& p = q.p;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g4 = lane >> 4;
+    const int m0 = mt * (16 * MB), n0 = n_begin + wave * (16 * NC), n_first = min(n0, p.N - 1);
+    const int steps = (p.K + 127) / 128, i0 = int(int64_t(steps) * split / splits), i1 = int(int64_t(steps) * (split + 1) / splits), h1 = 2 * i1;
+    const unsigned char* const base[2] = {p.w + size_t(n_first) * p.row_bytes, SW ? p.w2 + size_t(n_first) * p.row_bytes : nullptr};
+    const __amdgpu_buffer_rsrc_t sbase[2] = {__builtin_amdgcn_make_buffer_rsrc((void*)p.s, 0, p.groups * p.N * 2, 0x00020000),
+                                             __builtin_amdgcn_make_buffer_rsrc((void*)(SW ? p.s2 : p.s), 0, p.groups * p.N * 2, 0x00020000)};
+    unsigned row[NC], place[NC];
+#pragma unroll
+    for (int t = 0; t < NC; ++t) {
+        place[t] = min(n0 + 16 * t + n16, p.N - 1) - n_first;
+        row[t] = place[t] * p.row_bytes;
+    }
+    auto unit_of = [&](int t) { return q.out_unit[(t / NC) * p.N + n_first + place[t % NC]]; };
+    float per_unit[NT];                                         // what a scale is multiplied by
+#pragma unroll
+    for (int t = 0; t < NT; ++t) per_unit[t] = power(254 - int(__float_as_uint(unit_of(t)) >> 23));
+    uint4 w[WS][NT];
+    unsigned short s[WS][NT];
+    auto load = [&](int f, int i) {
+        const unsigned at = min(i * 64 + g4 * 16, p.row_bytes - 16);
+        const int g = min((i * 128 + g4 * 32) >> q.shift, p.groups - 1) * p.N + n_first;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            w[f][t] = *(const uint4*)(base[t / NC] + (row[t % NC] + at));
+            s[f][t] = __builtin_amdgcn_raw_buffer_load_b16(sbase[t / NC], (g + place[t % NC]) * 2, 0, 0);
+        }
+    };
+    // buffer loads: the compiler counts them as what they are, where it waits for loads into registers
+    const __amdgpu_buffer_rsrc_t xs = __builtin_amdgcn_make_buffer_rsrc(q.x, 0, steps * 256 * q.m_pad, 0x00020000);
+    const int x_from = wave * (DMA * 1024) + lane * 16;
+    auto bring = [&](int h) {                                   // half step h into its place in the ring
+        const int from = (min(h, h1 - 1) * q.m_pad + m0) * 128;
+        CAKE_LDS_AS void* const to = (CAKE_LDS_AS void*)(lds + (h & 3) * STAGE + wave * (DMA * 1024));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 0, 0);
+        if constexpr (DMA > 1) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 1024, 0);
+        if constexpr (DMA > 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 2048, 0);
+        if constexpr (DMA > 3) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 3072, 0);
+    };
+    const int get[2] = {n16 * 128 + ((g4 ^ (n16 >> 1 & 7)) << 4), n16 * 128 + (((4 + g4) ^ (n16 >> 1 & 7)) << 4)};
+    f32x4 acc[MB][NT];
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f16x8 x[MB];
+    f16x2 sc[NT];
+    auto scales = [&](int f) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const _Float16 y = _Float16(__uint_as_float(unsigned(s[f][t]) << 16) * per_unit[t]);
+            sc[t] = f16x2{y, y * _Float16(-24.f)};
+        }
+    };
+    // The products of eight inputs a lane, word j of the codes; behind the last tile's, the operands of what follows.
+    auto products = [&](int f, int j, int stage, int half) {
+        f16x8 o = weights8(word(w[f][0], j), sc[0]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            f16x8 next;
+            if (t + 1 < NT) next = weights8(word(w[f][t + 1 < NT ? t + 1 : t], j), sc[t + 1 < NT ? t + 1 : t]);
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                acc[b][t] = mfma16h(x[b], o, acc[b][t]);
+                if (t == NT - 1) x[b] = *(const f16x8*)(lds + stage * STAGE + b * 2048 + get[half]);
+            }
+            o = next;
+        }
+    };
+    if (i0 < i1) {
+#pragma unroll
+        for (int h = 0; h < 3; ++h) bring(2 * i0 + h);
+#pragma unroll
+        for (int f = 0; f < WS; ++f) load(f, min(i0 + f, i1 - 1));
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NT * WS + 2 * DMA) : "memory");
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int b = 0; b < MB; ++b) x[b] = *(const f16x8*)(lds + ((2 * i0) & 3) * STAGE + b * 2048 + get[0]);
+        auto step = [&](auto f_, int i) {
+            constexpr int f = decltype(f_)::value;
+            scales(f);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int h = 2 * i + half;
+                products(f, 2 * half, h & 3, 1);
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DMA + 2 * NT) : "memory");
+                __builtin_amdgcn_s_barrier();
+                bring(h + 3);
+                __builtin_amdgcn_sched_barrier(0);
+                products(f, 2 * half + 1, (h + 1) & 3, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            load(f, min(i + WS, i1 - 1));
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int i = i0;
+        for (; i + WS <= i1; i += WS) {
+            step(std::integral_constant<int, 0>{}, i);
+            step(std::integral_constant<int, 1>{}, i + 1);
+            if constexpr (WS == 4) {
+                step(std::integral_constant<int, 2>{}, i + 2);
+                step(std::integral_constant<int, 3>{}, i + 3);
+            }
+        }
+        if (i < i1) step(std::integral_constant<int, 0>{}, i);
+        if constexpr (WS == 4) {
+            if (i + 1 < i1) step(std::integral_constant<int, 1>{}, i + 1);
+            if (i + 2 < i1) step(std::integral_constant<int, 2>{}, i + 2);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what was asked for past the end
+    }
+    float unit[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) unit[t] = unit_of(t);
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+        const f32x4 ru = *(const f32x4*)(q.row_unit + m0 + 16 * b + 4 * g4);
+        const auto value = [&](int t, int v) { return acc[b][t][v] * ru[v] * unit[t]; };
+#pragma unroll
+        for (int t = 0; t < NC; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int m = m0 + 16 * b + 4 * g4 + v, n = n0 + 16 * t + n16;
+                if (m >= p.M || n >= p.N) continue;
+                const size_t at = size_t(m) * p.N + n;
+                const float y = value(t, v);
+                if (splits > 1) {
+                    float* d = p.parts + size_t(split) * (SW ? 2 : 1) * p.M * p.N + at;
+                    *d = y;
+                    if constexpr (SW) d[size_t(p.M) * p.N] = value(t + NC, v);
+                } else if constexpr (SW) ((bf16_t*)p.out)[at] = silu_product<bf16_t>(y, value(t + NC, v));
+                else if (p.epi == EPI_RESIDUAL_F32) ((float*)p.out)[at] += y;
+                else ((float*)p.out)[at] = y;
+            }
+    }
+}
+
+// Workgroups of two widths, so that a launch fills the compute units evenly: the first `more` of a row tile's `tiles` take 64 outputs more than the others.
+template <bool SW, int MB, int NT>
+__global__ void __launch_bounds__(256, 2)
+w4_wide_kernel(Wide q, int m_tiles, int tiles, int more, int splits) {
+    constexpr int U = SW ? 2 : 1, W = 64 * NT / U;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    const Place at = place_of(blockIdx.x, m_tiles);
+    if (at.column >= tiles * splits) return;
+    const int tile = at.column % tiles, split = at.column / tiles;
+    if constexpr (NT < 4)
+        if (tile < more) {
+            w4_wide_tile<SW, MB, NT + U>(q, lds, at.mt, tile * (W + 64), split, splits);
+            return;
+        }
+    w4_wide_tile<SW, MB, NT>(q, lds, at.mt, tile * W + more * 64, split, splits);
+}
+
 // The ranges' parts in their order.
+template <bool SW>
 __global__ void __launch_bounds__(256)
 w4_parts_kernel(Product p, int splits) {
-    const size_t size = size_t(p.M) * p.N, stride = p.epi == EPI_SWIGLU ? 2 * size : size;
+    const size_t size = size_t(p.M) * p.N, stride = SW ? 2 * size : size;
     for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < size; i += size_t(gridDim.x) * 256) {
         float y = 0.f, y2 = 0.f;
+#pragma unroll 8
         for (int q = 0; q < splits; ++q) {
             y += p.parts[q * stride + i];
-            if (p.epi == EPI_SWIGLU) y2 += p.parts[q * stride + size + i];
+            if constexpr (SW) y2 += p.parts[q * stride + size + i];
         }
-        if (p.epi == EPI_SWIGLU) ((bf16_t*)p.out)[i] = silu_product<bf16_t>(y, y2);
+        if constexpr (SW) ((bf16_t*)p.out)[i] = silu_product<bf16_t>(y, y2);
         else if (p.epi == EPI_RESIDUAL_F32) ((float*)p.out)[i] += y;
         else ((float*)p.out)[i] = y;
     }
@@ -460,6 +728,7 @@ hipError_t rows(const Product& p, hipStream_t st) {
     const std::integral_constant<int, 3> three{};
     const std::integral_constant<int, 4> four{};
     const std::integral_constant<int, 8> eight{};
+    const std::integral_constant<int, 16> sixteen{};
     if constexpr (sizeof(T) == 4) {
         if constexpr (SW) return go(two, one, eight);
         else return go(one, one, eight);
@@ -467,47 +736,93 @@ hipError_t rows(const Product& p, hipStream_t st) {
         int nt = forced("W4_NT"), v = forced("W4_V");
         if (!nt) nt = SW ? 2 : 1;
         if constexpr (!SW)
-            if (nt == 1) return v == 1 ? go(one, four, eight) : v == 2 ? go(one, two, four) : v == 3 ? go(one, four, four) : go(one, two, eight);
-        if (nt == 2) return v == 1 ? go(two, three, eight) : v == 2 ? go(two, two, four) : v == 3 ? go(two, three, four) : go(two, two, eight);
-        return v == 1 ? go(four, one, eight) : v == 2 ? go(four, two, four) : v == 3 ? go(four, one, four) : go(four, two, eight);
+            if (nt == 1) return v == 1 ? go(one, four, eight) : v == 2 ? go(one, two, sixteen) : v == 3 ? go(one, four, sixteen) : go(one, two, eight);
+        if (nt == 2) return v == 1 ? go(two, three, eight) : v == 2 ? go(two, two, sixteen) : v == 3 ? go(two, three, sixteen) : go(two, two, eight);
+        return v == 1 ? go(four, one, eight) : go(four, two, eight);
     }
 }
 
+template <bool SW>
+hipError_t add_parts(const Product& p, int splits, hipStream_t st) {
+    hipLaunchKernelGGL(w4_parts_kernel<SW>, dim3(unsigned(std::min<int64_t>((int64_t(p.M) * p.N + 255) / 256, 1 << 16))), dim3(256), 0, st, p, splits);
+    return hipGetLastError();
+}
+// How many parts of the result the workspace holds.
+inline int64_t parts_in(size_t bytes, const Product& p) { return int64_t(bytes / (size_t(p.M) * p.N * (p.epi == EPI_SWIGLU ? 8 : 4))); }
+
 template <bool SW, int GS>
 hipError_t tiles(Product p, float* ws, size_t ws_bytes, hipStream_t st) {
-    auto go = [&](auto mb, auto nt, auto ws_, auto xs) {
-        constexpr int MB = decltype(mb)::value, NT = decltype(nt)::value, NC = SW ? NT / 2 : NT;
-        const int m_tiles = (p.M + 16 * MB - 1) / (16 * MB), n_tiles = (p.N + 64 * NC - 1) / (64 * NC), steps = (p.K + 127) / 128;
-        const int64_t grid = int64_t(m_tiles) * n_tiles;
-        int splits = forced("W4_SPLIT");
-        if (!splits) splits = int(std::max<int64_t>(1, std::min<int64_t>(steps / 4, 512 / grid)));
-        splits = int(std::min<int64_t>(splits, int64_t(ws_bytes / (size_t(p.M) * p.N * (SW ? 8 : 4)))));
-        if (splits < 1) splits = 1;
+    auto go = [&](auto mb, auto ahead) {
+        constexpr int MB = decltype(mb)::value, NT = 2, LDS = 2 * MB * 16 * (256 + 128 / GS * 4);
+        const int m_tiles = (p.M + 16 * MB - 1) / (16 * MB), n_tiles = (p.N + 64 * (SW ? 1 : 2) - 1) / (64 * (SW ? 1 : 2)), steps = (p.K + 127) / 128;
+        int64_t splits = std::min<int64_t>(steps / 4, 512 / (int64_t(m_tiles) * n_tiles));
+        if (forced("W4_SPLIT")) splits = forced("W4_SPLIT");
+        splits = std::max<int64_t>(1, std::min(splits, parts_in(ws_bytes, p)));
         p.parts = ws;
-        constexpr int LDS = 2 * MB * 16 * (256 + 128 / GS * 4);
-        hipLaunchKernelGGL((w4_tile_kernel<SW, MB, NT, GS, decltype(ws_)::value, decltype(xs)::value>), dim3(unsigned((grid * splits + 7) / 8 * 8)), dim3(256), LDS, st, p, m_tiles,
-                           n_tiles, splits);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess || splits == 1) return e;
-        hipLaunchKernelGGL(w4_parts_kernel, dim3(unsigned(std::min<int64_t>((int64_t(p.M) * p.N + 255) / 256, 1 << 16))), dim3(256), 0, st, p, splits);
-        return hipGetLastError();
+        hipLaunchKernelGGL((w4_tile_kernel<SW, MB, NT, GS, decltype(ahead)::value, 2>), dim3(unsigned(blocks_of(int(n_tiles * splits), m_tiles))), dim3(256), LDS, st, p, m_tiles, n_tiles,
+                           int(splits));
+        const hipError_t e = hipGetLastError();
+        return e != hipSuccess || splits == 1 ? e : add_parts<SW>(p, int(splits), st);
     };
     const std::integral_constant<int, 1> one{};
     const std::integral_constant<int, 2> two{};
+    const std::integral_constant<int, 3> three{};
     const std::integral_constant<int, 4> four{};
-    int nt = forced("W4_NT"), mb = forced("W4_MB");
-    if (!mb) mb = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
-    if (!nt) nt = p.M <= 64 ? 2 : 4;
-    if (mb == 1) return go(one, two, two, two);
-    if (mb == 2) return go(two, two, two, two);
-    if (nt == 2) return go(four, two, two, two);
-    return go(four, four, one, one);
+    return p.M <= 16 ? go(one, four) : p.M <= 32 ? go(two, four) : p.M <= 48 ? go(three, two) : go(four, two);
+}
+
+template <bool SW>
+hipError_t wide(Product p, int group, float* ws, size_t ws_bytes, hipStream_t st) {
+    auto go = [&](auto mb, auto nt, int tiles, int more) {
+        constexpr int MB = decltype(mb)::value, NT = decltype(nt)::value, LDS = 4 * MB * 2048;
+        const int m_tiles = (p.M + 16 * MB - 1) / (16 * MB), steps = (p.K + 127) / 128;
+        Wide q;
+        q.m_pad = m_tiles * 16 * MB;
+        q.shift = group == 128 ? 7 : group == 64 ? 6 : 5;
+        unsigned char* at = (unsigned char*)ws;
+        q.x = (_Float16*)at; at += size_t(steps) * 2 * q.m_pad * 128;
+        q.row_unit = (float*)at; at += size_t(q.m_pad) * 4;
+        q.out_unit = (float*)at; at += (size_t(p.N) * (SW ? 2 : 1) * 4 + 15) / 16 * 16;
+        p.parts = (float*)at;
+        int64_t splits = std::min<int64_t>(steps / 24, 512 / (int64_t(m_tiles) * tiles));
+        if (forced("W4_SPLIT")) splits = forced("W4_SPLIT");
+        splits = std::max<int64_t>(1, std::min(splits, parts_in(ws_bytes - (at - (unsigned char*)ws), p)));
+        q.p = p;
+        hipLaunchKernelGGL(w4_prepare_kernel, dim3(unsigned(q.m_pad + (p.N + 63) / 64 * (SW ? 2 : 1))), dim3(256), 0, st, q);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((w4_wide_kernel<SW, MB, NT>), dim3(unsigned(blocks_of(int(tiles * splits), m_tiles))), dim3(256), LDS, st, q, m_tiles, tiles, more, int(splits));
+        e = hipGetLastError();
+        return e != hipSuccess || splits == 1 ? e : add_parts<SW>(p, int(splits), st);
+    };
+    const std::integral_constant<int, 4> four{};
+    const std::integral_constant<int, 8> eight{};
+    const int units = (p.N + 63) / 64, m_tiles = (p.M + 127) / 128;      // 64 outputs
+    int mb = forced("W4_MB");
+    if (!mb) mb = int64_t(p.M) * units >= 65536 && (p.M >= 512 || m_tiles * 2 == (p.M + 63) / 64) ? 8 : 4;
+    if (mb == 4) return go(four, std::integral_constant<int, SW ? 2 : 1>{}, units, 0);
+    // two workgroups a compute unit, in as few rounds as their widths allow
+    const int slots = std::max(1, 512 / m_tiles), most = SW ? 2 : 4, rounds = (units + slots * most - 1) / (slots * most);
+    const int tiles = std::min(units, rounds * slots), width = units / tiles, more = units - tiles * width;
+    if constexpr (SW) return width >= 2 ? go(eight, std::integral_constant<int, 4>{}, tiles, 0) : go(eight, std::integral_constant<int, 2>{}, tiles, more);
+    else return width >= 4 ? go(eight, std::integral_constant<int, 4>{}, tiles, 0) : width == 3 ? go(eight, std::integral_constant<int, 3>{}, tiles, more)
+              : width == 2 ? go(eight, std::integral_constant<int, 2>{}, tiles, more) : go(eight, std::integral_constant<int, 1>{}, tiles, more);
+}
+
+// What a many-rows launch needs of the workspace; 0: more than its offsets of 32 bits reach.
+inline size_t wide_bytes(const Product& p, int rows) {
+    const size_t pad = (size_t(rows) + 127) / 128 * 128, x = size_t((p.K + 127) / 128) * 256 * pad, n = size_t(p.N) * (p.epi == EPI_SWIGLU ? 2 : 1);
+    return x >= size_t(1) << 31 || size_t(p.groups) * p.N * 2 >= size_t(1) << 31 ? 0 : x + pad * 4 + n * 4 + 16;
 }
 
 template <typename T, bool SW, int GS>
 hipError_t choose(const Product& p, float* ws, size_t ws_bytes, hipStream_t st) {
-    if constexpr (sizeof(T) == 2)
-        if ((forced("W4_K") == 2 || (!forced("W4_K") && p.M > 16))) return tiles<SW, GS>(p, ws, ws_bytes, st);
+    if constexpr (sizeof(T) == 2) {
+        const int k = forced("W4_K");
+        const size_t need = wide_bytes(p, p.M);
+        if (need && need <= ws_bytes && (k == 3 || (!k && int64_t(p.M) * p.N * (SW ? 2 : 1) >= 800000 && p.M > 64))) return wide<SW>(p, GS, ws, ws_bytes, st);
+        if (k == 2 || (!k && p.M > 4)) return tiles<SW, GS>(p, ws, ws_bytes, st);
+    }
     return rows<T, SW, GS>(p, st);
 }
 
