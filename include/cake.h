@@ -664,8 +664,11 @@ typedef struct {
 int32_t cake_op_pack_w4(cake_ctx* ctx, const void* w, void* codes, void* scales, void* values, int32_t N, int32_t K, int32_t group);
 /* The products of cake_op_gemm, cake_op_gemm_residual and cake_op_gemm_swiglu with such weights: a[M][K] (device, model dtype, 16-byte aligned),
  *   out[M][N] (float32) = a w^T;   x[M][N] (float32) += a w^T;   out[M][N] (model dtype) = silu(a gate^T) * (a up^T), gate and up of one size.
- * Activations and codes are multiplied as they are and added up in float32; a group's sum is multiplied by its scale in float32.  The sum over
- * the groups may be taken in another order for other M.  M <= 2^20; N and K <= 2^20.  The result must not overlap what is read.
+ * Activations and codes are multiplied as they are and added up in float32; a group's sum is multiplied by its scale in float32.  With many rows
+ * (bf16 models; more than 64, and 800 000 results or more) the scale is multiplied into the codes first, exactly for scales down to 2^-27 of their output's largest
+ * and activations down to 2^-31 of their row's largest, and smaller ones lose at most 2^-35 and 2^-39 of the largest.  The order of the sums
+ * depends on M and on the context's size.  bf16 models: a result whose row holds an infinity, or activations beyond 2^115, may be a NaN
+ * where a sum of plain products would be infinite.  M, N and K <= 2^20, M N <= 2^35.  The result must not overlap what is read.
  * Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_gemm_w4(cake_ctx* ctx, const void* a, const cake_w4* w, float* out, int32_t M);
 int32_t cake_op_gemm_w4_residual(cake_ctx* ctx, const void* a, const cake_w4* w, float* x, int32_t M);

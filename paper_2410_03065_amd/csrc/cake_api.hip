@@ -1650,7 +1650,7 @@ static int gemm_w4(cake_ctx* c, const char* what, int epi, const void* a, const 
         if (rc == CAKE_OK && (w2->n != w->n || w2->k != w->k || w2->group != w->group)) rc = fail(c, CAKE_E_INVAL, "%s: gate and up of different sizes", what);
     }
     if (rc != CAKE_OK) return rc;
-    if (M < 0 || M > W4_MOST) return fail(c, CAKE_E_INVAL, "%s: %d rows", what, M);
+    if (M < 0 || M > W4_MOST || int64_t(M) * w->n > int64_t(1) << 35) return fail(c, CAKE_E_INVAL, "%s: %d rows of %d outputs", what, M, w->n);
     if (M == 0) return CAKE_OK;
     if (!a || !out || off16(a) || uintptr_t(out) % (epi == EPI_SWIGLU && c->m.dtype == CAKE_BF16 ? 2 : 4)) return fail(c, CAKE_E_INVAL, "%s: activations or result null or not aligned", what);
     const OnDevice on(c->device);

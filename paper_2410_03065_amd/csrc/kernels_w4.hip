@@ -2,10 +2,11 @@
 //
 // out[m][n] = sum over groups g of s[n][g] * (sum over the group's k of a[m][k] c[n][k]): the matrix cores multiply the activations by the
 // codes, exact in bfloat16, a group's sum is kept apart and enters the result times its scale, one multiply-add.  Nothing is rounded
-// on the way but float32 sums.
+// on the way but float32 sums.  With many rows those multiply-adds cost more than the products, and the scale goes into the weight instead.
+//
+// Up to some 100 rows the codes' bytes bound it, then the conversion of the codes, and from 500 rows on the matrix cores.
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <type_traits>
 
 #include "kernels.hpp"
@@ -80,17 +81,22 @@ __device__ __forceinline__ bf16x8 minus24() { return __builtin_bit_cast(bf16x8, 
 
 // Few rows.  A wave takes 16 NT outputs and an NW-th of the inputs in steps of 128, PF steps of codes ahead; a lane's 16 bytes of a row's codes
 // are 32 inputs of it.  Groups of 128: the four lanes of a row multiply their first eight, second eight .. at once.  Shorter groups: the
-// lanes exchange words first, so that a product's 32 inputs lie in one group.
-template <typename T, bool SW, int NT, int GS, int NW, int PF>
+// lanes exchange words first, so that a product's 32 inputs lie in one group.  The activations of R rows lie in LDS, in pieces of eight in the order
+// of the codes: loads come back in order, and one of a row's that waits behind the codes would take their depth away.  They are brought for
+// `held` steps at a time, all of them where they fit.  Measured: one row, gate and up of 14336 outputs and 4096 inputs, 14.4 us, 4.2 TB/s of 60.6 MB
+// (a plain read of as many bytes takes 10 us); 28672 outputs 13.1 us; 4096 outputs of 14336 inputs 8.6 us.  With the rows read from memory where they
+// are used instead: 17.6 us.
+template <typename T, bool SW, int R, int NT, int GS, int NW, int PF>
 __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 4 : 2)
-w4_rows_kernel(Product p) {
+w4_rows_kernel(Product p, int held) {
     constexpr int TERMS = Terms<T>::N, NC = SW ? NT / 2 : NT, PER = 128 / GS, MFMAS = 4 / PER;   // NC: tiles of outputs; PER: groups a step
     constexpr bool OFFSET = sizeof(T) == 2;
     static_assert(!SW || NT % 2 == 0, "gate and up side by side");
     __shared__ float part[NW][NT][4][64];
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];     // [step][term][16 pieces][R rows] of 16 bytes
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g4 = lane >> 4;
-    const int n0 = blockIdx.x * (16 * NC), m0 = blockIdx.y * 16;
-    const int steps = (p.K + 127) / 128, i0 = steps * wave / NW, i1 = steps * (wave + 1) / NW;
+    const int n0 = blockIdx.x * (16 * NC), m0 = blockIdx.y * R;
+    const int steps = (p.K + 127) / 128;
     // Rows past the last: the last, not stored; codes and scales past a row's end: its last, whose activations are zero.
     const unsigned char* const base[2] = {p.w + size_t(n0) * p.row_bytes, SW ? p.w2 + size_t(n0) * p.row_bytes : nullptr};
     const T* const sbase[2] = {(const T*)p.s + n0, SW ? (const T*)p.s2 + n0 : nullptr};
@@ -100,10 +106,6 @@ w4_rows_kernel(Product p) {
         place[t] = min(n0 + 16 * t + n16, p.N - 1) - n0;
         row[t] = place[t] * p.row_bytes;
     }
-    const bool mine = m0 + n16 < p.M;                 // a lane whose row is past the last asks for nothing
-    const T* const abase = (const T*)p.a + size_t(m0) * p.K;
-    const unsigned arow = (mine ? n16 : 0) * p.K;
-
     uint4 w[PF][NT];
     T s[PF][NT][PER];
     auto load = [&](int f, int i) {
@@ -115,44 +117,16 @@ w4_rows_kernel(Product p) {
             for (int g = 0; g < PER; ++g) s[f][t][g] = (sbase[t / NC] + size_t(min(i * PER + g, p.groups - 1)) * p.N)[place[t % NC]];
         }
     };
-    typedef typename std::conditional<TERMS == 1, uint4, f32x4[2]>::type Raw;
-    Raw raw[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (TERMS == 1) raw[j] = uint4{0, 0, 0, 0};
-        else raw[j][0] = raw[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    auto load_rows = [&](int i) {
-        if (mine)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = i * 128 + (GS == 128 ? 32 * g4 + 8 * j : 32 * j + 8 * g4);
-                const T* from = abase + (arow + unsigned(min(k, p.K - 8)));
-                if constexpr (TERMS == 1) raw[j] = *(const uint4*)from;
-                else { raw[j][0] = *(const f32x4*)from; raw[j][1] = *(const f32x4*)(from + 4); }
-            }
-    };
     f32x4 acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto step = [&](int f, int i) {
+    auto step = [&](int f, int i, int first, int last) {
         bf16x8 x[TERMS][4];
-        const bool whole = i * 128 + 128 <= p.K;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bool past = !whole && i * 128 + (GS == 128 ? 32 * g4 + 8 * j : 32 * j + 8 * g4) >= p.K;
-            if constexpr (TERMS == 1) {
-                x[0][j] = in_order(past ? uint4{0, 0, 0, 0} : raw[j]);
-            } else {
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float y = past ? 0.f : raw[j][e >> 2][e & 3];
-#pragma unroll
-                    for (int q = 0; q < TERMS; ++q) { x[q][j][e] = bf16_t(y); y -= float(x[q][j][e]); }
-                }
-            }
-        }
-        load_rows(min(i + 1, i1 - 1));
+            for (int q = 0; q < TERMS; ++q)
+                x[q][j] = *(const bf16x8*)(lds + ((((i - first) * TERMS + q) * 16 + (GS == 128 ? 4 * g4 + j : 4 * j + g4)) * R + n16 % R) * 16);
         if constexpr (GS < 128)
 #pragma unroll
             for (int t = 0; t < NT; ++t) w[f][t] = transposed(w[f][t]);
@@ -178,16 +152,38 @@ w4_rows_kernel(Product p) {
                 for (int v = 0; v < 4; ++v) acc[t][v] = __builtin_fmaf(sum[t][v], sc, acc[t][v]);
             }
         }
-        load(f, min(i + PF, i1 - 1));
+        load(f, min(i + PF, last - 1));
     };
-    if (i0 < i1) {
+    for (int first = 0; first < steps; first += held) {
+        const int n = min(held, steps - first), i0 = first + n * wave / NW, i1 = first + n * (wave + 1) / NW;
+        if (i0 < i1)
 #pragma unroll
-        for (int f = 0; f < PF; ++f) load(f, min(i0 + f, i1 - 1));
-        load_rows(i0);
+            for (int f = 0; f < PF; ++f) load(f, min(i0 + f, i1 - 1));
+        if (first) __syncthreads();
+        for (int i = threadIdx.x; i < n * 16 * R; i += 64 * NW) {
+            const int r = i / (n * 16), c = i % (n * 16), k = first * 128 + c * 8;          // neighbouring pieces of a row
+            const T* const from = (const T*)p.a + size_t(min(m0 + r, p.M - 1)) * p.K + min(k, p.K - 8);
+            unsigned char* const to = lds + ((c / 16 * TERMS * 16 + c % 16) * R + r) * 16;
+            if constexpr (TERMS == 1) {
+                *(bf16x8*)to = in_order(k < p.K ? *(const uint4*)from : uint4{0, 0, 0, 0});
+            } else {
+                const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
+                bf16x8 x[TERMS];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float y = k < p.K ? (e < 4 ? lo[e] : hi[e - 4]) : 0.f;
+#pragma unroll
+                    for (int q = 0; q < TERMS; ++q) { x[q][e] = bf16_t(y); y -= float(x[q][e]); }
+                }
+#pragma unroll
+                for (int q = 0; q < TERMS; ++q) *(bf16x8*)(to + q * 16 * R * 16) = x[q];
+            }
+        }
+        __syncthreads();
         for (int i = i0; i < i1; i += PF)
 #pragma unroll
             for (int f = 0; f < PF; ++f)
-                if (i + f < i1) step(f, i + f);
+                if (i + f < i1) step(f, i + f, first, i1);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -195,9 +191,9 @@ w4_rows_kernel(Product p) {
         for (int v = 0; v < 4; ++v) part[wave][t][v][lane] = acc[t][v];
     __syncthreads();
     // the waves' parts in their order; D[4 g4 + v][n16]
-    for (int i = threadIdx.x; i < NC * 256; i += 64 * NW) {
-        const int l = i & 63, v = i >> 6 & 3, t = i >> 8;
-        const int m = m0 + 4 * (l >> 4) + v, n = n0 + 16 * t + (l & 15);
+    for (int i = threadIdx.x; i < NC * 16 * R; i += 64 * NW) {
+        const int r = i / (NC * 16), c = i % (NC * 16), t = c / 16, l = r / 4 * 16 + c % 16, v = r % 4;
+        const int m = m0 + r, n = n0 + c;
         float y = 0.f, y2 = 0.f;
 #pragma unroll
         for (int q = 0; q < NW; ++q) {
@@ -217,6 +213,8 @@ w4_rows_kernel(Product p) {
 // tiles, rows of 256 bytes whose 16-byte pieces lie at piece ^ row, so that 16 rows' pieces of one number lie in different banks.  Who brings a
 // piece also adds up its activations, for -24 times the sum of a row's group: where a group's sum begins.
 // A unit is a group of a tile of 16 outputs.  While its products run, the next unit's codes are converted and the last one's sums scaled.
+// Bound by the time from a load to its use: a launch's workgroups live for a few steps, and the ranges are joined by a second launch (3 to 4 us).
+// Measured: 33 rows, 4096 outputs of 14336 inputs, groups of 64: 19.5 us, 1.6 TB/s.
 template <bool SW, int MB, int NT, int GS, int WS, int XS>
 __device__ __forceinline__ void w4_tile(const Product& p, unsigned char* lds, int mt, int n_begin, int split, int splits) {
     constexpr int NC = SW ? NT / 2 : NT, PER = 128 / GS, MF = 4 / PER, UNITS = PER * NT, TILE = MB * 16 * 256, SUMS = PER * MB * 16 * 4;
@@ -400,8 +398,8 @@ __device__ __forceinline__ f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) { return __b
 struct Wide {
     Product p;
     _Float16* x;            // [2 steps][m_pad][64]
-    float* row_unit;        // [m_pad]
-    float* out_unit;        // [2][N]: 2^(E - 10)
+    int* row_unit;          // [m_pad]: exponents of the units
+    int* out_unit;          // [2][N]
     int m_pad, shift;       // 2^shift inputs share a scale
 };
 __device__ __forceinline__ float power(int biased) { return __uint_as_float(unsigned(biased) << 23); }
@@ -424,7 +422,7 @@ w4_prepare_kernel(Wide q) {
         }
         top[tid] = most;
         __syncthreads();
-        if (tid < 64 && n < p.N) q.out_unit[which * p.N + n] = power(max(int(max(max(most, top[tid + 64]), max(top[tid + 128], top[tid + 192])) >> 7), 11) - 10);
+        if (tid < 64 && n < p.N) q.out_unit[which * p.N + n] = max(int(max(max(most, top[tid + 64]), max(top[tid + 128], top[tid + 192])) >> 7), 11) - 137;
         return;
     }
     const int m = int(blockIdx.x) - of_outputs, chunks = (p.K + 127) / 128 * 16;
@@ -449,7 +447,7 @@ w4_prepare_kernel(Wide q) {
     __syncthreads();
     const int e = max(int(max(max(top[0], top[1]), max(top[2], top[3])) >> 7), 15);
     const float f = power(268 - e);                             // 2^(14 - (e - 127))
-    if (tid == 0) q.row_unit[m] = power(e - 14);
+    if (tid == 0) q.row_unit[m] = e - 141;
     auto put = [&](int c, uint4 v) {
         const int k = 8 * c, r = k & 127, slot = ((r >> 3 & 1) * 4 + (r >> 5)) ^ (m >> 1 & 7);
         f16x8 h;
@@ -477,12 +475,14 @@ __device__ __forceinline__ f16x8 weights8(unsigned w, f16x2 s) {
 }
 
 // A workgroup takes 16 MB rows and 64 NC outputs (SwiGLU: of each matrix), a wave all of the rows and 16 NC outputs.  Activations come into LDS in
-// halves of a step, a ring of four, by loads that pass no register; codes into registers, a step ahead.  Half-way through a half step all its
-// operands are read: there the waves meet, the next half must have come, and the third from here is asked for, into the place of the last.
+// halves of a step, a ring of RING, by loads that pass no register; codes into registers, steps ahead.  Half-way through a half step all its
+// operands are read: there the waves meet, the next half must have come, and the last of the ring is asked for, into the place of the half before.
+// Loads come back in order, so the ring has to reach as far ahead as the codes.  Measured: 1024 rows, 10240 outputs of 8192 inputs: 148 us, 1.16
+// PFLOP/s, of the 1.20 that a library's large bfloat16 product reaches here; 11 us more for the pass before.
 #define CAKE_LDS_AS __attribute__((address_space(3)))
 template <bool SW, int MB, int NT>
 __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, int mt, int n_begin, int split, int splits) {
-    constexpr int NC = SW ? NT / 2 : NT, STAGE = MB * 2048, DMA = MB / 2, WS = MB < 8 ? 4 : 2;   // WS: steps of codes on their way
+    constexpr int NC = SW ? NT / 2 : NT, STAGE = MB * 2048, DMA = MB / 2, WS = MB < 8 ? 4 : 2, RING = 4;   // WS: steps of codes on their way
     static_assert(!SW || NT % 2 == 0, "gate and up side by side");
     static_assert(MB % 2 == 0, "a stage in whole loads of each wave");
     const Product& p = q.p;
@@ -501,7 +501,7 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
     auto unit_of = [&](int t) { return q.out_unit[(t / NC) * p.N + n_first + place[t % NC]]; };
     float per_unit[NT];                                         // what a scale is multiplied by
 #pragma unroll
-    for (int t = 0; t < NT; ++t) per_unit[t] = power(254 - int(__float_as_uint(unit_of(t)) >> 23));
+    for (int t = 0; t < NT; ++t) per_unit[t] = power(127 - unit_of(t));
     uint4 w[WS][NT];
     unsigned short s[WS][NT];
     auto load = [&](int f, int i) {
@@ -518,7 +518,7 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
     const int x_from = wave * (DMA * 1024) + lane * 16;
     auto bring = [&](int h) {                                   // half step h into its place in the ring
         const int from = (min(h, h1 - 1) * q.m_pad + m0) * 128;
-        CAKE_LDS_AS void* const to = (CAKE_LDS_AS void*)(lds + (h & 3) * STAGE + wave * (DMA * 1024));
+        CAKE_LDS_AS void* const to = (CAKE_LDS_AS void*)(lds + h % RING * STAGE + wave * (DMA * 1024));
         __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 0, 0);
         if constexpr (DMA > 1) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 1024, 0);
         if constexpr (DMA > 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 2048, 0);
@@ -556,26 +556,26 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
     };
     if (i0 < i1) {
 #pragma unroll
-        for (int h = 0; h < 3; ++h) bring(2 * i0 + h);
+        for (int h = 0; h < RING - 1; ++h) bring(2 * i0 + h);
 #pragma unroll
         for (int f = 0; f < WS; ++f) load(f, min(i0 + f, i1 - 1));
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NT * WS + 2 * DMA) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NT * WS + (RING - 2) * DMA) : "memory");
         __builtin_amdgcn_s_barrier();
 #pragma unroll
-        for (int b = 0; b < MB; ++b) x[b] = *(const f16x8*)(lds + ((2 * i0) & 3) * STAGE + b * 2048 + get[0]);
+        for (int b = 0; b < MB; ++b) x[b] = *(const f16x8*)(lds + 2 * i0 % RING * STAGE + b * 2048 + get[0]);
         auto step = [&](auto f_, int i) {
             constexpr int f = decltype(f_)::value;
             scales(f);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int h = 2 * i + half;
-                products(f, 2 * half, h & 3, 1);
+                products(f, 2 * half, h % RING, 1);
                 __builtin_amdgcn_sched_barrier(0);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DMA + 2 * NT) : "memory");
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 3) * DMA + (RING - 2) * NT) : "memory");
                 __builtin_amdgcn_s_barrier();
-                bring(h + 3);
+                bring(h + RING - 1);
                 __builtin_amdgcn_sched_barrier(0);
-                products(f, 2 * half + 1, (h + 1) & 3, 0);
+                products(f, 2 * half + 1, (h + 1) % RING, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
             load(f, min(i + WS, i1 - 1));
@@ -597,13 +597,13 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what was asked for past the end
     }
-    float unit[NT];
+    int unit[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) unit[t] = unit_of(t);
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
-        const f32x4 ru = *(const f32x4*)(q.row_unit + m0 + 16 * b + 4 * g4);
-        const auto value = [&](int t, int v) { return acc[b][t][v] * ru[v] * unit[t]; };
+        const int4 ru = *(const int4*)(q.row_unit + m0 + 16 * b + 4 * g4);
+        const auto value = [&](int t, int v) { return ldexpf(acc[b][t][v], (v == 0 ? ru.x : v == 1 ? ru.y : v == 2 ? ru.z : ru.w) + unit[t]); };
 #pragma unroll
         for (int t = 0; t < NC; ++t)
 #pragma unroll
@@ -714,32 +714,35 @@ pack_w4_kernel(const T* __restrict__ w, unsigned char* __restrict__ codes, T* __
     }
 }
 
-int forced(const char* name) { const char* e = getenv(name); return e ? atoi(e) : 0; }
-
+// Waves that share a workgroup's inputs.  Bytes on their way are waves times the codes each has asked for: where a launch has workgroups
+// enough, fewer waves with longer ways waste less on beginning and joining; where it has few and the inputs are long, more waves.  One row, 4 / 8 / 16
+// waves, us: 28672 outputs of 4096 inputs 13.1 / 15.1 / -, 8192 of 4096 7.0 / 6.3 / 6.5, 4096 of 14336 17.2 / 11.3 / 9.6.
 template <typename T, bool SW, int GS>
 hipError_t rows(const Product& p, hipStream_t st) {
-    auto go = [&](auto nt, auto pf, auto nw) {
-        constexpr int NT = decltype(nt)::value, NC = SW ? NT / 2 : NT, PF = decltype(pf)::value, NW = decltype(nw)::value;
-        hipLaunchKernelGGL((w4_rows_kernel<T, SW, NT, GS, NW, PF>), dim3(unsigned((p.N + 16 * NC - 1) / (16 * NC)), unsigned((p.M + 15) / 16)), dim3(64 * NW), 0, st, p);
-        return hipGetLastError();
+    constexpr int NT = SW ? 2 : 1;
+    auto go = [&](auto r, auto nw) {
+        constexpr int R = decltype(r)::value, PF = sizeof(T) == 2 ? 2 : 1, NW = decltype(nw)::value, STEP = Terms<T>::N * 256 * R;
+        const int held = std::min((p.K + 127) / 128, (sizeof(T) == 2 ? 32 << 10 : 24 << 10) / STEP);
+        constexpr int MOST = 65535 * R;                    // a grid's second size
+        for (int m = 0; m < p.M; m += MOST) {
+            Product q = p;
+            q.M = std::min(p.M - m, MOST);
+            q.a = (const T*)p.a + size_t(m) * p.K;
+            q.out = (char*)p.out + size_t(m) * p.N * (SW ? sizeof(T) : sizeof(float));
+            hipLaunchKernelGGL((w4_rows_kernel<T, SW, R, NT, GS, NW, PF>), dim3(unsigned((p.N + 15) / 16), unsigned((q.M + R - 1) / R)), dim3(64 * NW), held * STEP, st, q, held);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+        return hipSuccess;
     };
-    const std::integral_constant<int, 1> one{};
-    const std::integral_constant<int, 2> two{};
-    const std::integral_constant<int, 3> three{};
-    const std::integral_constant<int, 4> four{};
-    const std::integral_constant<int, 8> eight{};
-    const std::integral_constant<int, 16> sixteen{};
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (SW) return go(two, one, eight);
-        else return go(one, one, eight);
-    } else {
-        int nt = forced("W4_NT"), v = forced("W4_V");
-        if (!nt) nt = SW ? 2 : 1;
-        if constexpr (!SW)
-            if (nt == 1) return v == 1 ? go(one, four, eight) : v == 2 ? go(one, two, sixteen) : v == 3 ? go(one, four, sixteen) : go(one, two, eight);
-        if (nt == 2) return v == 1 ? go(two, three, eight) : v == 2 ? go(two, two, sixteen) : v == 3 ? go(two, three, sixteen) : go(two, two, eight);
-        return v == 1 ? go(four, one, eight) : go(four, two, eight);
-    }
+    auto by_waves = [&](auto r) {
+        const std::integral_constant<int, 8> eight{};
+        if constexpr (sizeof(T) == 4) return go(r, eight);
+        else {
+            const int n = (p.N + 15) / 16 * NT;
+            return n > 1024 ? go(r, std::integral_constant<int, 4>{}) : n > 256 || p.K < 8192 ? go(r, eight) : go(r, std::integral_constant<int, 16>{});
+        }
+    };
+    return p.M == 1 ? by_waves(std::integral_constant<int, 1>{}) : by_waves(std::integral_constant<int, 4>{});
 }
 
 template <bool SW>
@@ -756,7 +759,6 @@ hipError_t tiles(Product p, float* ws, size_t ws_bytes, hipStream_t st) {
         constexpr int MB = decltype(mb)::value, NT = 2, LDS = 2 * MB * 16 * (256 + 128 / GS * 4);
         const int m_tiles = (p.M + 16 * MB - 1) / (16 * MB), n_tiles = (p.N + 64 * (SW ? 1 : 2) - 1) / (64 * (SW ? 1 : 2)), steps = (p.K + 127) / 128;
         int64_t splits = std::min<int64_t>(steps / 4, 512 / (int64_t(m_tiles) * n_tiles));
-        if (forced("W4_SPLIT")) splits = forced("W4_SPLIT");
         splits = std::max<int64_t>(1, std::min(splits, parts_in(ws_bytes, p)));
         p.parts = ws;
         hipLaunchKernelGGL((w4_tile_kernel<SW, MB, NT, GS, decltype(ahead)::value, 2>), dim3(unsigned(blocks_of(int(n_tiles * splits), m_tiles))), dim3(256), LDS, st, p, m_tiles, n_tiles,
@@ -781,11 +783,10 @@ hipError_t wide(Product p, int group, float* ws, size_t ws_bytes, hipStream_t st
         q.shift = group == 128 ? 7 : group == 64 ? 6 : 5;
         unsigned char* at = (unsigned char*)ws;
         q.x = (_Float16*)at; at += size_t(steps) * 2 * q.m_pad * 128;
-        q.row_unit = (float*)at; at += size_t(q.m_pad) * 4;
-        q.out_unit = (float*)at; at += (size_t(p.N) * (SW ? 2 : 1) * 4 + 15) / 16 * 16;
+        q.row_unit = (int*)at; at += size_t(q.m_pad) * 4;
+        q.out_unit = (int*)at; at += (size_t(p.N) * (SW ? 2 : 1) * 4 + 15) / 16 * 16;
         p.parts = (float*)at;
         int64_t splits = std::min<int64_t>(steps / 24, 512 / (int64_t(m_tiles) * tiles));
-        if (forced("W4_SPLIT")) splits = forced("W4_SPLIT");
         splits = std::max<int64_t>(1, std::min(splits, parts_in(ws_bytes - (at - (unsigned char*)ws), p)));
         q.p = p;
         hipLaunchKernelGGL(w4_prepare_kernel, dim3(unsigned(q.m_pad + (p.N + 63) / 64 * (SW ? 2 : 1))), dim3(256), 0, st, q);
@@ -798,9 +799,10 @@ hipError_t wide(Product p, int group, float* ws, size_t ws_bytes, hipStream_t st
     const std::integral_constant<int, 4> four{};
     const std::integral_constant<int, 8> eight{};
     const int units = (p.N + 63) / 64, m_tiles = (p.M + 127) / 128;      // 64 outputs
-    int mb = forced("W4_MB");
-    if (!mb) mb = int64_t(p.M) * units >= 65536 && (p.M >= 512 || m_tiles * 2 == (p.M + 63) / 64) ? 8 : 4;
-    if (mb == 4) return go(four, std::integral_constant<int, SW ? 2 : 1>{}, units, 0);
+    // 128 rows or 64: a workgroup's codes are converted once for its rows, but 64 make twice the workgroups, and up to 512 rows less padding.
+    // 128 against 64 rows, us: 1024 rows, 10240 outputs of 8192 inputs 162 / 243; 512, 4096 of 4096 40.1 / 35.0; 320, 14336 of 4096 76 / 64;
+    // 512, 14336 of 4096 76 / 87; 128, 28672 of 4096 49 / 53.
+    if (int64_t(p.M) * units < 65536 || (p.M < 512 && m_tiles * 2 != (p.M + 63) / 64)) return go(four, std::integral_constant<int, SW ? 2 : 1>{}, units, 0);
     // two workgroups a compute unit, in as few rounds as their widths allow
     const int slots = std::max(1, 512 / m_tiles), most = SW ? 2 : 4, rounds = (units + slots * most - 1) / (slots * most);
     const int tiles = std::min(units, rounds * slots), width = units / tiles, more = units - tiles * width;
@@ -818,10 +820,16 @@ inline size_t wide_bytes(const Product& p, int rows) {
 template <typename T, bool SW, int GS>
 hipError_t choose(const Product& p, float* ws, size_t ws_bytes, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
-        const int k = forced("W4_K");
+        const int64_t outputs = int64_t(p.N) * (SW ? 2 : 1);
+        // Few rows: each four read the weights once more, which come from a cache then, but there is one launch and nothing between its workgroups.
+        // rows / tiles, us: 4 rows, 4096 outputs of 4096 inputs 5.3 / 8.3, 16384 of 4096 10.8 / 13.0, 8192 of 8192 15.0 / 12.5, 28672 of 6144
+        // 32.7 / 24.9; 8 rows, 6144 of 4096 8.7 / 10.4, 12288 of 4096 15.5 / 13.3; 32 rows, 2048 of 2048 6.2 / 10.0; 16 rows, 4096 of 4096 9.1 / 8.6.
+        if (p.M == 1 || (p.M <= 4 && p.K <= 4096) || (p.M + 3) / 4 * outputs * p.K < int64_t(1) << 26) return rows<T, SW, GS>(p, st);
+        // Many rows: the pass before the product costs some 8 us.  tiles / wide, us: 128 rows, 12288 outputs of 4096 inputs 36.4 / 28.9, 4096 of 14336
+        // 33.4 / 34.9; 512 rows, 4096 of 4096 37.9 / 33.9, 1792 of 2048 23.6 / 18.3; up to 64 rows a tile's codes are converted once.
         const size_t need = wide_bytes(p, p.M);
-        if (need && need <= ws_bytes && (k == 3 || (!k && int64_t(p.M) * p.N * (SW ? 2 : 1) >= 800000 && p.M > 64))) return wide<SW>(p, GS, ws, ws_bytes, st);
-        if (k == 2 || (!k && p.M > 4)) return tiles<SW, GS>(p, ws, ws_bytes, st);
+        if (p.M > 64 && p.M * outputs >= 800000 && need && need <= ws_bytes) return wide<SW>(p, GS, ws, ws_bytes, st);
+        return tiles<SW, GS>(p, ws, ws_bytes, st);
     }
     return rows<T, SW, GS>(p, st);
 }

@@ -204,6 +204,121 @@ def test_a_row_does_not_depend_on_those_beside_it_and_runs_repeat(kind, M):
     assert torch.equal(eng.op_gemm_w4(t, p.w4)[M // 2:], first[M // 2:])
 
 
+# ---------------------------------------------------------------------------------------------- choices between kernels
+def wide_loss(p, a):
+    """What many rows may lose more (a scale and an activation each rounded to a multiple of 2^-24 in units that put the largest of its output
+    at 2^10 or more, the largest of its row at 2^14 or more): codes are at most 8."""
+    most_a, most_s = np.abs(a).max(axis=1, keepdims=True), p.scales.astype(np.float64).max(axis=1)
+    return 2.0 ** -35 * 8 * np.abs(a).sum(axis=1, keepdims=True) * most_s + 2.0 ** -39 * most_a * np.abs(p.values).sum(axis=1)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(65, 12301, 264), (80, 10001, 1000), (129, 6208, 136), (128, 30000, 40), (300, 2667, 712), (513, 8200, 200), (512, 8192, 1024), (1030, 4100, 72), (65, 12308, 4104)])
+def test_many_rows(group, M, N, K):
+    """At least 800 000 results: weights in half precision; 64 and 128 rows a workgroup, one to four tiles wide, inputs in one range and in several."""
+    check_plain("bf16", M, N, K, group)
+
+
+@pytest.mark.parametrize("form", ["residual", "swiglu"])
+@pytest.mark.parametrize("M,N,K,group", [(65, 6200, 264, 32), (70, 12309, 5000, 128), (128, 33000, 72, 64), (513, 9001, 200, 128), (520, 17000, 136, 64)])
+def test_many_rows_residual_and_swiglu(form, M, N, K, group):
+    import torch
+    eng = engine("bf16")
+    gate, up = Projection(eng, N, K, group, 1), Projection(eng, N, K, group, 2)
+    t, a = activations(eng, M, K)
+    if form == "residual":
+        x = torch.randn((M, N), device="cuda", generator=torch.Generator("cuda").manual_seed(M))
+        before = x.double().cpu().numpy()
+        want = before + a @ gate.values.T
+        got = eng.op_gemm_w4_residual(t, gate.w4, x).double().cpu().numpy()
+        assert (np.abs(got - want) <= gate.bound(a, "bf16") + 2.0 ** -24 * (np.abs(want) + np.abs(before))).all()
+        return
+    g, u = a @ gate.values.T, a @ up.values.T
+    want, dg, du = serving.silu_product(g, u), gate.bound(a, "bf16"), up.bound(a, "bf16")
+    # as in test_residual_and_swiglu
+    bound = 2.0 ** -8 * np.abs(want) + 1.1 * dg * (np.abs(u) + du) + np.abs(g) * du + 2.0 ** -20 * np.abs(want) * (1 + np.abs(g) / 16) + 1e-37
+    assert (np.abs(eng.op_gemm_w4_swiglu(t, gate.w4, up.w4).double().cpu().numpy() - want) <= bound).all()
+
+
+@pytest.mark.parametrize("M,N", [(3, 70), (40, 90), (70, 12000), (520, 9000)])
+def test_scales_and_activations_of_very_different_size(M, N):
+    """Scales over 2^40 within an output, outputs over 2^60, activations over 2^40 within a row, rows over 2^60; an output and a row of zeros."""
+    import torch
+    eng, K, group = engine("bf16"), 520, 64
+    rng = np.random.default_rng([M, N])
+    scales = 2.0 ** (rng.integers(-40, 1, (N, 9)) + rng.integers(-40, 21, (N, 1)))
+    scales[N // 2] = 0
+    p = Projection(eng, N, K, group, scales=scales.astype(np.float32))
+    a = rng.standard_normal((M, K)) * 2.0 ** (rng.integers(-40, 1, (M, K)) + rng.integers(-20, 41, (M, 1)))
+    a[M // 2] = 0
+    t = torch.from_numpy(a.astype(np.float32)).cuda().to(torch.bfloat16)
+    a = t.double().cpu().numpy()
+    off = np.abs(eng.op_gemm_w4(t, p.w4).double().cpu().numpy() - a @ p.values.T)
+    assert (off <= p.bound(a, "bf16") + (wide_loss(p, a) if M > 64 else 0)).all()
+
+
+def test_many_rows_at_the_ends_of_the_range():
+    """Activations of 2^100 against scales of 2^-90, of 2^-110 against 2^100, of 2^-120 against 2^-20: results in the middle and below the range."""
+    import torch
+    eng, M, N, K = engine("bf16"), 66, 12200, 136
+    rng = np.random.default_rng(8)
+    for big_a, big_s in ((100, -90), (-110, 100), (-120, -20), (-131, 100), (100, -131)):
+        p = Projection(eng, N, K, 128, scales=(2.0 ** big_s * rng.uniform(1, 2, (N, 2))).astype(np.float32))
+        t = torch.from_numpy((rng.standard_normal((M, K)) * 2.0 ** big_a).astype(np.float32)).cuda().to(torch.bfloat16)
+        a = t.double().cpu().numpy()
+        off = np.abs(eng.op_gemm_w4(t, p.w4).double().cpu().numpy() - a @ p.values.T)
+        assert (off <= p.bound(a, "bf16") + wide_loss(p, a)).all(), (big_a, big_s)
+
+
+@pytest.mark.parametrize("M,N", [(70, 12000), (520, 9000)])
+def test_many_rows_values_that_are_not_finite(M, N):
+    import torch
+    eng = engine("bf16")
+    p = Projection(eng, N, 296, 64)
+    t, _ = activations(eng, M, 296)
+    clean = eng.op_gemm_w4(t, p.w4).clone()
+    t[1, 5], t[M - 1, 295] = float("nan"), float("inf")
+    p.w4.scales[33, 2], p.w4.scales[N - 1, 0] = float("nan"), float("inf")
+    got = eng.op_gemm_w4(t, p.w4)
+    rows, outputs = torch.ones(M, dtype=torch.bool, device="cuda"), torch.ones(N, dtype=torch.bool, device="cuda")
+    rows[[1, M - 1]], outputs[[33, N - 1]] = False, False
+    assert not torch.isfinite(got[~rows]).any() and not torch.isfinite(got[:, ~outputs]).any()
+    assert torch.equal(got[rows][:, outputs], clean[rows][:, outputs])
+
+
+@pytest.mark.parametrize("M,N,K,group", [(2, 3000, 16392, 128), (1, 4112, 20000, 32), (40, 200, 9000, 64), (40, 8200, 4096, 128), (9, 10000, 2056, 32)])
+def test_few_rows_of_long_inputs_and_many_outputs(M, N, K, group):
+    """Activations in several parts through LDS; inputs in ranges; four, eight and sixteen waves."""
+    check_plain("bf16", M, N, K, group)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_the_most_rows(kind):
+    import torch
+    eng = engine(kind)
+    M, N, K = 2 ** 20, 3, 8
+    p = Projection(eng, N, K, 32)
+    t = torch.randn((M, K), device="cuda").to(eng.tdtype)
+    a = t.double().cpu().numpy()
+    got = eng.op_gemm_w4(t, p.w4).double().cpu().numpy()
+    assert (np.abs(got - a @ p.values.T) <= p.bound(a, kind)).all()
+    out = eng.op_gemm_w4_swiglu(t, p.w4, p.w4).double().cpu().numpy()
+    y = a @ p.values.T
+    want = serving.silu_product(y, y)
+    assert (np.abs(out - want) <= (2.0 ** -8 if kind == "bf16" else 2.0 ** -20) * (1 + np.abs(y)) * np.abs(want) + 4 * p.bound(a, kind) * (1 + np.abs(y))).all()
+
+
+def test_a_small_workspace():
+    """A context whose workspace holds neither the activations of many rows nor several parts of the result."""
+    import torch
+    eng = small_engine(4, 2, 64, "bf16")
+    for M, N, K in ((70, 11500, 16400), (600, 2000, 4096), (64, 8200, 4096)):
+        p = Projection(eng, N, K, 128)
+        t, a = activations(eng, M, K)
+        off = np.abs(eng.op_gemm_w4(t, p.w4).double().cpu().numpy() - a @ p.values.T)
+        assert (off <= p.bound(a, "bf16")).all()
+
+
 # ---------------------------------------------------------------------------------------------- packing
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("N,K,group", [(1, 8, 32), (3, 40, 32), (17, 128, 128), (5, 688, 32), (70, 712, 64), (130, 1000, 128), (1000, 256, 64), (257, 4096, 128)])
@@ -311,7 +426,7 @@ def test_graph_replays_beside_eager_calls(M):
 def test_two_graphs_of_one_context_in_turn():
     import torch
     eng, made = engine("bf16"), []
-    for M, N, K in ((1, 256, 8192), (40, 300, 4096), (130, 140, 2048)):
+    for M, N, K in ((1, 256, 8192), (40, 300, 4096), (130, 140, 2048), (66, 12160, 520), (70, 12000, 392)):
         p = Projection(eng, N, K, 128)
         t, _ = activations(eng, M, K)
         out = eng.op_gemm_w4(t, p.w4)
