@@ -5,7 +5,7 @@
 // it lies in.  A score is therefore (q . c_j) * s_j and an output sum_j (p_j s'_j) c'_j: the products run on the codes as they
 // are, exact in bfloat16 (eight bits), and a scale is one factor per score.  No dequantised copy of the cache exists anywhere.
 // Codes of 4 bits enter as 16 c, signed bytes whose upper half is the code: two masks make eight of them, and what follows is as
-// for 8 bits.  The factor 1 / 16 goes into the scales.
+// for 8 bits.  The factor 1 / 16 goes into the scales.  Few rows of bfloat16: as 24 + c (attention_kernel).
 #pragma once
 #include <algorithm>
 #include <atomic>
@@ -40,6 +40,16 @@ __device__ __forceinline__ bf16x8 nibbles8(unsigned w) {
     const uint4 r = {pack_hi(code(e, 0), code(o, 0)), pack_hi(code(e, 1), code(o, 1)), pack_hi(code(e, 2), code(o, 2)), pack_hi(code(e, 3), code(o, 3))};
     return __builtin_bit_cast(bf16x8, r);
 }
+// Eight 4-bit codes as bfloat16 24 + c, a shift and a three-way logic instruction a pair: a code's four bits, the upper one turned, are the
+// upper bits of the fraction of 16 .. 31.  Here of the four of each half of a word, pair j element j of both.
+__device__ __forceinline__ unsigned pair24(unsigned w, int j) {
+    return ((j == 0 ? w << 3 : w >> (4 * j - 3)) & 0x00780078u) ^ 0x41c041c0u;
+}
+__device__ __forceinline__ bf16x8 eight24(unsigned w) {      // elements 0 4 1 5 2 6 3 7
+    return __builtin_bit_cast(bf16x8, uint4{pair24(w, 0), pair24(w, 1), pair24(w, 2), pair24(w, 3)});
+}
+__device__ __forceinline__ bf16x8 in_pairs(bf16x8 x) { return __builtin_shufflevector(x, x, 0, 4, 1, 5, 2, 6, 3, 7); }      // the same order
+__device__ __forceinline__ bf16x8 eight_of(unsigned pair) { return __builtin_bit_cast(bf16x8, uint4{pair, pair, pair, pair}); }
 // What a scale is multiplied by, for codes that enter the products as they do.
 template <int BITS> constexpr float UNIT = BITS == 8 ? 1.f : 0.0625f;
 // The largest code.
@@ -379,7 +389,11 @@ template <int W> __device__ __forceinline__ KeySteps<W> key_steps(int pos_lo, in
 // its conversions pick the bytes, so nothing is transposed.  Bound by the cache's bytes; per byte 1.5 vector instructions.
 // Weights go to the product as two bfloat16 values each (16 bits; float32 models: three, all 24, as the queries): at this
 // size the matrix cores are idle, and a single bfloat16 would double the output's rounding error.
+// Codes of 4 bits enter as 24 + c: two instructions a pair, and four where they are widened to signed bytes first.  A score begins at -24 times the query's
+// sum, and 24 times the weights' sums, one more product a step, are taken from the outputs at the end: the same numbers in float32 but for
+// roundings of 24 times a wave's sum of weights, below 2^-24 24 of it each, where a bfloat16 output's own is 2^-8 of it.
 // Measured: 64 sequences of 500 to 8191 keys, 8 KV heads of 128: 126 us, 4.7 TB/s; 24 of 4100 visible keys, 32 KV heads: 147 us, 5.5 TB/s.
+// 4 bits: 84 us (as 16 c 98), 3.6 TB/s; 32 of 30001 keys 228 us (259), 4.6 TB/s; one of 100001 30 us (with the merge), 3.6 TB/s.
 template <typename T> struct Terms { static constexpr int Q = 1, W = 2; };
 template <> struct Terms<float> { static constexpr int Q = 3, W = 3; };
 
@@ -390,6 +404,8 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
     constexpr int TQ = Terms<T>::Q, TW = Terms<T>::W;
     constexpr int QC = HD / 32, CW = HD / 16, KE = HD / 4, HB = HD * BITS / 8;   // products per 16 keys; value columns and key elements per lane; a head's bytes
     constexpr int KB = KE * BITS / 8, KR = (KB + 15) / 16;
+    constexpr bool BY24 = BITS == 4 && TQ == 1;      // codes enter as 24 + c; float32 models: 16 c, exact, since the offset would cost their sums five bits
+    constexpr float VALUE_UNIT = BY24 ? 1.f : UNIT<BITS>;
     __shared__ float s_acc[4][16][HD + 4], s_ml[4][16][2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n16 = lane & 15, g4 = lane >> 4;
     unsigned b = blockIdx.x;
@@ -419,6 +435,7 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
             for (int c = 0; c < QC; ++c) {
                 if constexpr (TQ == 1) {
                     qf[r][0][c] = *(const bf16x8*)(p + 8 * c);
+                    if constexpr (BY24) qf[r][0][c] = in_pairs(qf[r][0][c]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -429,13 +446,17 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
                 }
             }
         }
-        f32x4 acc[NB][CW];
+        f32x4 acc[NB][CW], begin[NB], sums[NB];    // begin: what a score starts from, sums: of the weights
         float m[NB], l[NB];
 #pragma unroll
         for (int r = 0; r < NB; ++r) {
             m[r] = -FLT_MAX; l[r] = 0.f;
 #pragma unroll
             for (int j = 0; j < CW; ++j) acc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            begin[r] = sums[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (BY24)
+#pragma unroll
+                for (int c = 0; c < QC; ++c) begin[r] = mfma16(eight_of(0xc1c0c1c0u), qf[r][0][c], begin[r]);     // -24 times the query's sum
         }
         // One step's raw bytes: the next step's keys are asked for when these have been multiplied, its values likewise, so a
         // wave has a step in flight while it works, in half the registers of two sets (and twice the waves).
@@ -495,7 +516,7 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int r = 0; r < NB; ++r) sc[r][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int r = 0; r < NB; ++r) sc[r][h] = BY24 ? begin[r] : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < QC; ++c) {
                     bf16x8 kf;
@@ -504,7 +525,8 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
                         kf = c & 1 ? codes8(w.z, w.w) : codes8(w.x, w.y);
                     } else {
                         const uint4 w = kr[h][0];
-                        kf = nibbles8(c == 0 ? w.x : c == 1 ? w.y : c == 2 ? w.z : w.w);
+                        const unsigned y = c == 0 ? w.x : c == 1 ? w.y : c == 2 ? w.z : w.w;
+                        if constexpr (BY24) kf = eight24(y); else kf = nibbles8(y);
                     }
 #pragma unroll
                     for (int t = TQ - 1; t >= 0; --t)
@@ -539,6 +561,7 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
                     l[r] *= f;
 #pragma unroll
                     for (int j = 0; j < CW; ++j) acc[r][j] *= f;
+                    if constexpr (BY24) sums[r] *= f;
                     m[r] = top;
                 }
 #pragma unroll
@@ -548,16 +571,31 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
                         const float p = __builtin_amdgcn_exp2f(sc[r][h][e] - top);
                         l[r] += p;
                         // a hidden key's scale may be anything: memory behind the last token
-                        float w = edge && sc[r][h][e] == -INFINITY ? 0.f : p * (vsc[h][e % NS] * UNIT<BITS>);
+                        float w = edge && sc[r][h][e] == -INFINITY ? 0.f : p * (vsc[h][e % NS] * VALUE_UNIT);
 #pragma unroll
                         for (int t = 0; t < TW; ++t) { wf[r][t][4 * h + e] = bf16_t(w); w -= float(wf[r][t][4 * h + e]); }
                     }
             }
+            unsigned half[2][4];                   // BY24: of the lower and of the upper four columns, two keys' in a word
+            if constexpr (BY24) {
+#pragma unroll
+                for (int r = 0; r < NB; ++r)
+#pragma unroll
+                    for (int t = TW - 1; t >= 0; --t) sums[r] = mfma16(eight_of(0x41c041c0u), wf[r][t], sums[r]);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    half[0][t] = __builtin_amdgcn_perm(vr[2 * t + 1].x, vr[2 * t].x, 0x05040100);
+                    if constexpr (CW == 8) half[1][t] = __builtin_amdgcn_perm(vr[2 * t + 1].x, vr[2 * t].x, 0x07060302);
+                }
+            }
 #pragma unroll
             for (int j = 0; j < CW; ++j) {
                 uint4 a;
+                if constexpr (BY24) a = uint4{pair24(half[j / 4][0], j & 3), pair24(half[j / 4][1], j & 3), pair24(half[j / 4][2], j & 3), pair24(half[j / 4][3], j & 3)};
                 auto col = [&](int t) { return BITS == 8 ? code(j < 4 ? vr[t].x : vr[t].y, j & 3) : nibble(vr[t].x, j); };
-                a.x = pack_hi(col(0), col(1)); a.y = pack_hi(col(2), col(3)); a.z = pack_hi(col(4), col(5)); a.w = pack_hi(col(6), col(7));
+                if constexpr (!BY24) {
+                    a.x = pack_hi(col(0), col(1)); a.y = pack_hi(col(2), col(3)); a.z = pack_hi(col(4), col(5)); a.w = pack_hi(col(6), col(7));
+                }
                 const bf16x8 vf = __builtin_bit_cast(bf16x8, a);
 #pragma unroll
                 for (int r = 0; r < NB; ++r)
@@ -570,6 +608,9 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
 #pragma unroll
         for (int r = 0; r < NB; ++r) {
             if (r) __syncthreads();
+            if constexpr (BY24)
+#pragma unroll
+                for (int j = 0; j < CW; ++j) acc[r][j] -= sums[r];      // every column's; of one whose codes are zeros the same roundings, so nothing stays
             float lt = sum4(l[r]);
             auto leave = [&](int w) {
                 if (g4 == 0) { s_ml[w][n16][0] = m[r]; s_ml[w][n16][1] = lt; }
@@ -1051,6 +1092,72 @@ merge_kernel(const float* __restrict__ part, T* __restrict__ out, Q8View v, int 
     *(typename Vec<T, E>::type*)(out + i * HD + e0) = ov;
 }
 
+// The same sums in the same order, for few rows of many ranges: a workgroup takes 32 elements of a row, all of whose ranges are asked for at once, 256 at a time.
+// 32 rows of 241 ranges: 10 us, and 54 from memory in order, where a range waits for the one four before.  Whole rows to a workgroup: 30.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256)
+merge_long_kernel(const float* __restrict__ part, T* __restrict__ out, Q8View v, int n_q, int splits) {
+    constexpr int C = 256, E = 32, N = E / 4;                  // ranges at a time, elements; float4 of a thread
+    __shared__ __attribute__((aligned(16))) float x[C][E];
+    __shared__ float2 weight[C];
+    __shared__ float tops[4];
+    __shared__ int lasts[4];
+    const size_t i = blockIdx.x / (HD / E);
+    const int tid = threadIdx.x, e0 = blockIdx.x % (HD / E) * E, row = int(i / n_q);
+    if (row < v.row_begin[0] || row >= min(v.row_begin[v.n_seqs], v.n_rows)) return;
+    const float* p = part + i * splits * (HD + 4);
+    float4 next[N];
+    float2 ml;
+    auto load = [&](int base) {                 // past the last: the last again, not used
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (base + C / N * k < splits) next[k] = *(const float4*)(p + size_t(min(base + tid / N + C / N * k, splits - 1)) * (HD + 4) + e0 + tid % N * 4);
+        ml = *(const float2*)(p + size_t(min(base + tid, splits - 1)) * (HD + 4) + HD);
+    };
+    load(0);
+    float m = ml.x;
+    int used = ml.y != 0.f ? min(tid + 1, splits) : 0;
+    for (int s = tid + C; s < splits; s += C) {
+        const float2 y = *(const float2*)(p + size_t(s) * (HD + 4) + HD);
+        m = fmaxf(m, y.x);
+        if (y.y != 0.f) used = s + 1;
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        m = fmaxf(m, __shfl_xor(m, d));
+        used = max(used, __shfl_xor(used, d));
+    }
+    if ((tid & 63) == 0) { tops[tid >> 6] = m; lasts[tid >> 6] = used; }
+    __syncthreads();
+    m = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), -FLT_MAX);
+    used = max(max(lasts[0], lasts[1]), max(lasts[2], lasts[3]));
+    float sum = 0.f, o = 0.f;
+    for (int base = 0; base < used; base += C) {
+        if (base) __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) *(float4*)&x[tid / N + C / N * k][tid % N * 4] = next[k];
+        weight[tid] = base + tid < used ? make_float2(__builtin_amdgcn_exp2f(ml.x - m), ml.y) : make_float2(0.f, 0.f);
+        __syncthreads();
+        if (base + C < used) load(base + C);
+        if (tid < E) {
+            const int n = min(C, used - base);
+            for (int s = 0; s < n; s += 16) {                  // read before they are used: one after the other each would wait for LDS
+                float2 w[16];
+                float y[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) { w[k] = weight[s + k]; y[k] = x[s + k][tid]; }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    sum += w[k].y * w[k].x;
+                    o += w[k].y == 0.f ? 0.f : y[k] * w[k].x;
+                }
+            }
+        }
+    }
+    if (tid < E) out[i * HD + e0 + tid] = to_elem<T>(o * (sum == 0.f ? 0.f : 1.f / sum));
+}
+
 // A sequence's tiles beyond the launch's go round again, so a hint that is too small costs time and one that is too large none.
 constexpr int MOST_GROUPS = 1 << 18;
 
@@ -1105,7 +1212,15 @@ template <typename T>
 hipError_t merge(const Q8View& v, int n_q, const KeyRanges& k, const AttnWs& ws, T* out, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || k.splits == 1) return e;
-    const dim3 grid(unsigned((size_t(v.n_rows) * n_q + 15) / 16));
+    const size_t rows = size_t(v.n_rows) * n_q;
+    // With many ranges of few rows the way through LDS (us, attention and this, 4 bits, 8 KV heads of 128, against a lane's eight elements in order from
+    // memory): 32 rows, 241 ranges 43, 87; 32, 71 12.9, 24.9; 32, 32 9.1, 13.0; 256, 235 64, 90; 128, 64 44, 52; 256, 32 82, 78; 512, 32 104, 93.
+    if (k.splits > 8 && rows * v.head_dim <= size_t(512) * k.splits) {
+        if (v.head_dim == 128) hipLaunchKernelGGL((merge_long_kernel<T, 128>), dim3(unsigned(rows * 4)), dim3(256), 0, st, ws.part, out, v, n_q, k.splits);
+        else hipLaunchKernelGGL((merge_long_kernel<T, 64>), dim3(unsigned(rows * 2)), dim3(256), 0, st, ws.part, out, v, n_q, k.splits);
+        return hipGetLastError();
+    }
+    const dim3 grid(unsigned((rows + 15) / 16));
     if (v.head_dim == 128) hipLaunchKernelGGL((merge_kernel<T, 128>), grid, dim3(256), 0, st, ws.part, out, v, n_q, k.splits);
     else hipLaunchKernelGGL((merge_kernel<T, 64>), grid, dim3(256), 0, st, ws.part, out, v, n_q, k.splits);
     return hipGetLastError();
@@ -1113,7 +1228,13 @@ hipError_t merge(const Q8View& v, int n_q, const KeyRanges& k, const AttnWs& ws,
 
 template <int BITS, typename T, int HD, int NB, int NS>
 hipError_t attention(const T* q, T* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws, hipStream_t st) {
-    const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, 2048, ws);
+    if (BITS == 4 && Terms<T>::Q == 1) scale /= UNIT<BITS>;         // codes as 24 + c, not 16 c
+    // Of 4 bits, half the bytes a step, a workgroup's beginning and its part of the result weigh more: one round of workgroups, where the sequences'
+    // lengths do not differ.  512 / 768 / 1024 / 2048 (us, heads of 128): 1 of 100001 35.4, 29.6, 32.5, 38.6; 2 of 60001 36.3, 32.6, 37.7, 39.0; 4 of
+    // 500 to 30001 34.9, 31.4, 29.3, 33.1; 16 of 500 to 9001 32.5, 32.4, 28.8, 31.3; tiles of 32 rows: 1 of 60001 41.2, 41.8, 46.7, 63.8; 4 of 500
+    // to 30001 44, 56, 55, 61; heads of 64: 1 of 100001 28.4, 23.8, 24.0, 29.9.
+    const int want = BITS == 8 ? 2048 : NB == 2 ? 512 : HD == 128 && v.n_seqs <= 2 ? 768 : 1024;
+    const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, want, ws);
     // Undivided on eight waves, without a merge, where sequences are not too long for it: one such workgroup fills a compute unit, so the
     // steps that may be walked by one grow with the share of the 256 units that the last of up to two rounds fills.  Measured (us,
     // against four waves, divided, with the merge; a token each, 8 KV heads of 128, then of 64; sequences x keys): 1 x 300 7.5, 9.0;
@@ -1187,7 +1308,8 @@ hipError_t launch_attention(int dtype, const void* q, void* out, const Q8View& v
             if (eight <= few) return attention_rows<BITS, HD, 8, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
         // Heads of 64, half the bytes and products at the same other work: 1 of 16000: 192 rows 42, 45, 48; 512 rows 85, 66, 73;
         // 1024 rows 159, 109, 123; 4 of 4096: 512 rows 61, 74, 83; 1024 rows 111, 133, 133; 16 of 8191: 256 rows 194, 242, 327.
-        } else if (rows >= 512) {
+        // 4 bits: 1 of 16000: 128 rows 26, 33; 256 rows 44, 37; 16 of 8191, 256 rows 259, 160.
+        } else if (rows >= (BITS == 8 ? 512 : 256)) {
             return attention_rows<BITS, HD, 4, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
         }
         return attention<BITS, bf16_t, HD, 1, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);

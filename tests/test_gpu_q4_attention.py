@@ -21,6 +21,29 @@ def run(b, window=0, sinks=0, seed=0, q8=None, out=None):
     return q, got
 
 
+def bound_of(b, q, want, size, mass, reach, window=0, sinks=0):
+    """attention_bound, and what few rows of bf16 models add, whose codes enter as 24 + c, at most 31: a score is a sum of hd products of a
+    query's elements with those, begun at -24 times the elements' sum.  2 hd / 32 products of the matrix cores, each with at most 8 roundings of at
+    most 2^-24 of 31 times the query's magnitudes times the key's scale (reach of codes 1).  An output is a sum over a wave's keys, less 24 times the
+    weights' sum, another such sum: for every 32 keys two products each, 8 roundings, and one each where they are scaled, of 31 times the
+    weights' sum times the values' scales (the output of codes 1).  Four waves or more share at most 131 such steps of a range (48, where there are several): 131 / 8 and 48 / 4
+    are less than 17, and one more for what does not divide."""
+    s, most = b.eng.shape, int(max(b.lens.max(), 1))
+    bound = attention_bound(s.dtype, s.head_dim, want, size, mass, reach, most)
+    if s.dtype == "f32":
+        return bound
+    kept = b.pages.codes.copy()
+
+    def with_ones(which):
+        b.pages.codes[:, which] = 1
+        got = serving.attention(b.pages, q.double().cpu().numpy(), b.table, b.lens, b.begin, window, sinks)
+        b.pages.codes[:] = kept
+        return got
+    score = 2 * s.head_dim / 32 * 8 * 31 * 2.0 ** -24 * with_ones(0)[3][..., None]
+    steps = min(most / 128 + 1, 18)
+    return bound + 2 * size * np.expm1(score) + steps * (2 * 2 * 8 + 2) * 31 * 2.0 ** -24 * np.abs(with_ones(1)[0])
+
+
 def check(b, window=0, sinks=0, seed=0, q8=None):
     import torch
     s = b.eng.shape
@@ -30,7 +53,7 @@ def check(b, window=0, sinks=0, seed=0, q8=None):
     want, size, mass, reach = serving.attention(b.pages, q.double().cpu().numpy(), b.table, b.lens, b.begin, window, sinks)
     nobody = np.isnan(want)
     assert (got[nobody] == 77.0).all()
-    bound = attention_bound(s.dtype, s.head_dim, want, size, mass, reach, int(max(b.lens.max(), 1)))
+    bound = bound_of(b, q, want, size, mass, reach, window, sinks)
     off = np.abs(got - want)[~nobody]
     assert np.isfinite(got).all() and (off <= bound[~nobody]).all(), (off / bound[~nobody]).max()
     return got
@@ -146,16 +169,42 @@ def test_pages_outside_the_pool_and_lengths_beyond_the_table_are_not_followed(ro
     assert (run(b)[1][rows:2 * rows] == 0).all()
 
 
+@pytest.mark.parametrize("rows", [1, 63, 64, 65, 127, 128, 129])
+@pytest.mark.parametrize("length", [700, 3000])
+def test_heads_of_64_on_both_sides_of_the_tiles_choice(rows, length):
+    check(Batch(engine(8, 4, 64, "bf16"), [length, 130], [rows, min(rows, 65)], pt=64, block=4), seed=rows)
+    check(Batch(engine(8, 2, 64, "bf16"), [length], [rows], pt=64), window=300, sinks=2)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("kind,n_q,n_kv,hd", [("bf16", 4, 1, 128), ("f32", 2, 1, 128), ("bf16", 2, 1, 64), ("bf16", 2, 2, 64), ("f32", 3, 1, 64)])
+def test_hundreds_of_ranges(kind, n_q, n_kv, hd, bits):
+    """A few rows whose parts are joined 256 at a time: the last range full and short, ranges behind the last key, rows that see nothing, and
+    memory of earlier parts that must not be seen."""
+    import torch
+    eng = engine(n_q, n_kv, hd, kind)
+    b = AnyBatch(eng, [40001, 33], [1, 1], pt=256, block=64, bits=bits)
+    op = eng.op_attention_q4 if bits == 4 else eng.op_attention_q8
+    q = torch.from_numpy(np.random.default_rng(hd).standard_normal((n_q, 2, hd)).astype(np.float32)).cuda().to(eng.tdtype)
+    for window, sinks, length in ((0, 0, 40001), (0, 0, 33000), (20000, 70, 40001), (0, 0, 40), (0, 0, 0)):
+        b.lens[0] = length
+        b.d_lens[0] = length
+        got = op(q, 0, b.q8, window=window, sinks=sinks).double().cpu().numpy().reshape(2, n_q, hd)
+        want, size, mass, reach = serving.attention(b.pages, q.double().cpu().numpy(), b.table, b.lens, b.begin, window, sinks)
+        bound = bound_of(b, q, want, size, mass, reach, window, sinks) if bits == 4 else attention_bound(kind, hd, want, size, mass, reach, 40001)
+        assert np.isfinite(got).all() and (np.abs(got - want) <= bound).all(), (window, length)
+        assert length or (got[0] == 0).all()
+
+
 def test_scores_far_apart_and_equal():
     """Weights that vanish beside the largest, and a long run of equal ones."""
     import torch
     b = Batch(engine(4, 4, 64, "bf16"), [5000, 700], [1, 1], pt=64)
-    s = b.eng.shape
     q = torch.zeros((4, 2, 64), device="cuda", dtype=torch.bfloat16)
     q[:, 1] = 60.0
     got = b.eng.op_attention_q4(q, 0, b.q8).double().cpu().numpy().reshape(2, 4, 64)
     want, size, mass, reach = serving.attention(b.pages, q.double().cpu().numpy(), b.table, b.lens, b.begin)
-    assert (np.abs(got - want) <= attention_bound("bf16", s.head_dim, want, size, mass, reach, 5000)).all()
+    assert (np.abs(got - want) <= bound_of(b, q, want, size, mass, reach)).all()
 
 
 def test_scales_of_very_different_size():
