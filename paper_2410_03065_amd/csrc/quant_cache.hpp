@@ -18,6 +18,8 @@ namespace cake {
 namespace {
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
 // v_mfma_f32_16x16x32_bf16, D[16x16] += A[16x32] * B[32x16]: lane l supplies A[l%16][8*(l/16) .. +7] and
@@ -393,7 +395,9 @@ template <int W> __device__ __forceinline__ KeySteps<W> key_steps(int pos_lo, in
 // sum, and 24 times the weights' sums, one more product a step, are taken from the outputs at the end: the same numbers in float32 but for
 // roundings of 24 times a wave's sum of weights, below 2^-24 24 of it each, where a bfloat16 output's own is 2^-8 of it.
 // Measured: 64 sequences of 500 to 8191 keys, 8 KV heads of 128: 126 us, 4.7 TB/s; 24 of 4100 visible keys, 32 KV heads: 147 us, 5.5 TB/s.
-// 4 bits: 84 us (as 16 c 98), 3.6 TB/s; 32 of 30001 keys 228 us (259), 4.6 TB/s; one of 100001 30 us (with the merge), 3.6 TB/s.
+// 4 bits: 81 us (as 16 c 98), 3.7 TB/s; 32 of 30001 keys 219 us (259), 4.8 TB/s; one of 100001 28.5 us (with the merge), 3.8 TB/s.
+// With 4 bits the vector instructions weigh as much as the bytes: 33 sequences of 37 to 9001, 20 rows, a window of 4096, heads of 64, 33 us of
+// which they take 20.
 template <typename T> struct Terms { static constexpr int Q = 1, W = 2; };
 template <> struct Terms<float> { static constexpr int Q = 3, W = 3; };
 
@@ -564,16 +568,29 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
                     if constexpr (BY24) sums[r] *= f;
                     m[r] = top;
                 }
+                float w[8];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int i = 0; i < 8; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(sc[r][i / 4][i % 4] - top);
+                    l[r] += p;
+                    w[i] = p * (vsc[i / 4][i % 4 % NS] * VALUE_UNIT);
+                }
+                if (edge) {                            // a hidden key's scale may be anything: memory behind the last token
+                    asm volatile("");                  // a branch: as selects they cost every step two instructions a weight
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(sc[r][h][e] - top);
-                        l[r] += p;
-                        // a hidden key's scale may be anything: memory behind the last token
-                        float w = edge && sc[r][h][e] == -INFINITY ? 0.f : p * (vsc[h][e % NS] * VALUE_UNIT);
+                    for (int i = 0; i < 8; ++i) w[i] = sc[r][i / 4][i % 4] == -INFINITY ? 0.f : w[i];
+                }
 #pragma unroll
-                        for (int t = 0; t < TW; ++t) { wf[r][t][4 * h + e] = bf16_t(w); w -= float(wf[r][t][4 * h + e]); }
+                for (int t = 0; t < TW; ++t)
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {   // two at once
+                        const bf16x2 y = __builtin_convertvector(f32x2{w[i], w[i + 1]}, bf16x2);
+                        wf[r][t][i] = y[0]; wf[r][t][i + 1] = y[1];
+                        if (t + 1 < TW) {
+                            const unsigned both = __builtin_bit_cast(unsigned, y);
+                            w[i] -= __uint_as_float(both << 16);
+                            w[i + 1] -= __uint_as_float(both & 0xffff0000u);
+                        }
                     }
             }
             unsigned half[2][4];                   // BY24: of the lower and of the upper four columns, two keys' in a word
