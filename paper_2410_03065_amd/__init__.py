@@ -949,7 +949,7 @@ class Engine:
         n = codes.shape[0]
         at = self._operand(codes, "codes", self.torch.uint8, (n, (k + 31) // 32 * 16))
         self._operand(scales, "scales", self.tdtype, (n, (k + group - 1) // group))
-        return self._w4_of(codes, at, scales.t().contiguous(), n, k, group)
+        return self._w4_of(codes, at, scales.t().clone(memory_format=self.torch.contiguous_format), n, k, group)
 
     def _w4_of(self, codes, at, by_group, n, k, group):
         w = W4(at, by_group.data_ptr(), n, k, group)

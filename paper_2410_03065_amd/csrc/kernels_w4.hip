@@ -521,8 +521,8 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
         CAKE_LDS_AS void* const to = (CAKE_LDS_AS void*)(lds + h % RING * STAGE + wave * (DMA * 1024));
         __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 0, 0);
         if constexpr (DMA > 1) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 1024, 0);
-        if constexpr (DMA > 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 2048, 0);
-        if constexpr (DMA > 3) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 3072, 0);
+        if constexpr (DMA > 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 2 * 1024, 0);
+        if constexpr (DMA > 3) __builtin_amdgcn_raw_ptr_buffer_load_lds(xs, to, 16, x_from, from, 3 * 1024, 0);
     };
     const int get[2] = {n16 * 128 + ((g4 ^ (n16 >> 1 & 7)) << 4), n16 * 128 + (((4 + g4) ^ (n16 >> 1 & 7)) << 4)};
     f32x4 acc[MB][NT];

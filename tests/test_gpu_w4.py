@@ -292,6 +292,47 @@ def test_few_rows_of_long_inputs_and_many_outputs(M, N, K, group):
     check_plain("bf16", M, N, K, group)
 
 
+def check_swiglu(eng, M, N, K, group):
+    gate, up = Projection(eng, N, K, group, 1), Projection(eng, N, K, group, 2)
+    t, a = activations(eng, M, K)
+    g, u = a @ gate.values.T, a @ up.values.T
+    want, dg, du = serving.silu_product(g, u), gate.bound(a, "bf16"), up.bound(a, "bf16")
+    # as in test_residual_and_swiglu
+    bound = 2.0 ** -8 * np.abs(want) + 1.1 * dg * (np.abs(u) + du) + np.abs(g) * du + 2.0 ** -20 * np.abs(want) * (1 + np.abs(g) / 16) + 1e-37
+    assert (np.abs(eng.op_gemm_w4_swiglu(t, gate.w4, up.w4).double().cpu().numpy() - want) <= bound).all()
+
+
+@pytest.mark.parametrize("M,N,K,group", [(1, 1000, 16400, 128), (2, 1000, 8200, 64), (4, 2048, 8192, 32), (3, 2049, 8192, 128), (1, 8200, 1032, 128), (16, 300, 9000, 32)])
+def test_few_rows_gate_and_up(M, N, K, group):
+    """Four, eight and sixteen waves, the last with all of a workgroup's LDS."""
+    check_swiglu(engine("bf16"), M, N, K, group)
+
+
+@pytest.mark.parametrize("form", ["plain", "swiglu"])
+def test_many_rows_of_long_inputs(form):
+    """More inputs than the pass before the product keeps in registers, and ranges of them."""
+    eng = small_engine(32, 2, 64, "bf16")                      # a larger workspace
+    if form == "swiglu":
+        check_swiglu(eng, 300, 1400, 17000, 128)
+        return
+    p = Projection(eng, 2700, 17000, 64)
+    t, a = activations(eng, 300, 17000)
+    off = np.abs(eng.op_gemm_w4(t, p.w4).double().cpu().numpy() - a @ p.values.T)
+    assert (off <= p.bound(a, "bf16")).all()
+
+
+@pytest.mark.parametrize("N,K", [(1, 136), (5, 24)])
+def test_a_description_keeps_its_scales(N, K):
+    """One output, or one group: a layout in which the transposed scales are the scales themselves."""
+    import torch
+    eng = engine("bf16")
+    codes = torch.full((N, (K + 31) // 32 * 16), 0x11, dtype=torch.uint8, device="cuda")
+    scales = torch.ones((N, -(-K // 32)), dtype=torch.bfloat16, device="cuda")
+    w, a = eng.w4(codes, scales, K, 32), torch.ones((2, K), dtype=torch.bfloat16, device="cuda")
+    scales.zero_()
+    assert (eng.op_gemm_w4(a, w) == K).all()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_the_most_rows(kind):
     import torch
