@@ -622,7 +622,7 @@ int32_t cake_op_append_q8(cake_ctx* ctx, const float* qkv, void* q, void* values
 int32_t cake_op_attention_q8(cake_ctx* ctx, const void* q, void* out, int32_t layer, int32_t window, int32_t sinks,
                              const cake_q8_batch* batch);
 /* The two calls on pages of 4 bits: codes rounded to 7 steps of the scale either way, the rest as above, with 11 bits a weight for heads of 64
- * from 256 rows on; with fewer rows (either head size) bf16 models add up 24 + code in float32, and take the 24 off the sums.  A code of -8, which
+ * from 256 rows on; bf16 models add up 24 + code in float32 (the values' codes with few rows), and take the 24 off the sums.  A code of -8, which
  * append never writes, counts as what it says.  Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_append_q4(cake_ctx* ctx, const float* qkv, void* q, void* values, int32_t layer, const cake_rope* rope,
                           const cake_q4_batch* batch);

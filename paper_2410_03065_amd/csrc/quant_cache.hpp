@@ -5,7 +5,7 @@
 // it lies in.  A score is therefore (q . c_j) * s_j and an output sum_j (p_j s'_j) c'_j: the products run on the codes as they
 // are, exact in bfloat16 (eight bits), and a scale is one factor per score.  No dequantised copy of the cache exists anywhere.
 // Codes of 4 bits enter as 16 c, signed bytes whose upper half is the code: two masks make eight of them, and what follows is as
-// for 8 bits.  The factor 1 / 16 goes into the scales.  Few rows of bfloat16: as 24 + c (attention_kernel).
+// for 8 bits.  The factor 1 / 16 goes into the scales.  Few rows of bfloat16, and the keys of many: as 24 + c (attention_kernel).
 #pragma once
 #include <algorithm>
 #include <atomic>
@@ -702,7 +702,7 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
 // first of them before the barrier.
 // Bound by the vector instructions beside the products: a score takes 5 and an exponential (four times the issue of one), a
 // code 1.5 over the workgroup's rows.  1024 rows of 32 heads after 15360 keys, 8 KV heads of 128: 330 to 390 us with the clock, 0.7 to
-// 0.8 PFLOP/s; with products, weights and the rest each left alone, 131, 81 and 195.
+// 0.8 PFLOP/s; with products, weights and the rest each left alone, 131, 81 and 195.  4 bits: 307 us (keys as 16 c: 314).
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
 __device__ __forceinline__ f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -765,7 +765,18 @@ attention_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, fl
             pos[r] = i < n ? p0 + i / G : -1;
             const bf16_t* p = q + (size_t(g * G + (i < n ? i % G : 0)) * v.n_rows + seq.row0 + (i < n ? i / G : 0)) * HD + g4 * 8;
 #pragma unroll
-            for (int c = 0; c < QC; ++c) qf[r][c] = *(const bf16x8*)(p + 32 * c);
+            for (int c = 0; c < QC; ++c) {
+                qf[r][c] = *(const bf16x8*)(p + 32 * c);
+                if constexpr (BITS == 4) qf[r][c] = in_pairs(qf[r][c]);
+            }
+        }
+        f32x4 begin[2];                                       // 4 bits, keys as 24 + c: -24 times the queries' sums
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            begin[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (BITS == 4)
+#pragma unroll
+                for (int c = 0; c < QC; ++c) begin[r] = mfma16(eight_of(0xc1c0c1c0u), qf[r][c], begin[r]);
         }
         f32x4 acc[2][HB];
         float m[2] = {0.f, 0.f}, l[2] = {0.f, 0.f};
@@ -811,7 +822,7 @@ attention_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, fl
             unsigned char* base = lds + buf * L::TILE;
             if constexpr (decltype(keys_)::value) {
                 if constexpr (BITS == 8) *(bf16x8*)(base + (k_put ^ (c << 4))) = codes8(raw[2 * c], raw[2 * c + 1]);
-                else *(bf16x8*)(base + (k_put ^ (c << 4))) = nibbles8(raw[c]);
+                else *(bf16x8*)(base + (k_put ^ (c << 4))) = eight24(raw[c]);
             } else {
                 auto val = [&](int t) { return BITS == 8 ? code(VC == 8 ? raw[2 * t + c / 4] : raw[t], c & 3) : nibble(raw[t], c); };
                 const uint4 x = {pack_code(val(0), val(1)), pack_code(val(2), val(3)), pack_code(val(4), val(5)), pack_code(val(6), val(7))};
@@ -868,7 +879,7 @@ attention_rows_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, fl
                 for (int r = 0; r < 2; ++r) {
                     if (x < K) {
                         f32x4& d = sc[key_block(x)][r];
-                        d = mfma16(f[x % AHEAD], qf[r][key_part(x)], key_part(x) ? d : f32x4{0.f, 0.f, 0.f, 0.f});
+                        d = mfma16(f[x % AHEAD], qf[r][key_part(x)], key_part(x) ? d : BITS == 4 ? begin[r] : f32x4{0.f, 0.f, 0.f, 0.f});
                     } else {
                         f32x4& d = acc[r][value_block(x - K)];
                         d = mfma16h(__builtin_bit_cast(f16x8, f[x % AHEAD]), wf[r][value_part(x - K)], d);
@@ -1278,6 +1289,7 @@ hipError_t attention(const T* q, T* out, const Q8View& v, int n_q, int max_rows,
 template <int BITS, int HD, int NWV, int NS>
 hipError_t attention_rows(const bf16_t* q, bf16_t* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws,
                              hipStream_t st) {
+    if (BITS == 4) scale /= UNIT<BITS>;                        // keys as 24 + c, not 16 c
     const KeyRanges k = key_ranges(v, n_q, 32 * NWV, 64, max_rows, max_len, window, sinks, 4, 1 << 20, NWV == 8 ? 256 : 512, ws);
     constexpr int LDS = RowsLds<HD>::BYTES;
     static std::atomic<uint64_t> set{0};                       // a bit per device

@@ -22,7 +22,7 @@ def run(b, window=0, sinks=0, seed=0, q8=None, out=None):
 
 
 def bound_of(b, q, want, size, mass, reach, window=0, sinks=0):
-    """attention_bound, and what few rows of bf16 models add, whose codes enter as 24 + c, at most 31: a score is a sum of hd products of a
+    """attention_bound, and what bf16 models add, whose codes (with many rows the keys') enter as 24 + c, at most 31: a score is a sum of hd products of a
     query's elements with those, begun at -24 times the elements' sum.  2 hd / 32 products of the matrix cores, each with at most 8 roundings of at
     most 2^-24 of 31 times the query's magnitudes times the key's scale (reach of codes 1).  An output is a sum over a wave's keys, less 24 times the
     weights' sum, another such sum: for every 32 keys two products each, 8 roundings, and one each where they are scaled, of 31 times the
