@@ -369,6 +369,134 @@ __device__ __forceinline__ void w4_tile(const Product& p, unsigned char* lds, in
             }
 }
 
+// Many rows of float32 models.  As above, with three terms of each activation in LDS and two tiles of 16 rows; a code's conversion (twice a
+// bfloat16 one's instructions) serves 32 rows, a fragment of activations two tiles of outputs.  Bound by those conversions and by the time of a
+// step, some 1.2 us, while a launch has few workgroups.  Measured: 732 rows, 3553 outputs, 1320 inputs: 34 us, four rows at a time 188.
+template <bool SW, int GS>
+__global__ void __launch_bounds__(256, 2)
+w4_f32_kernel(Product p) {
+    constexpr int MB = 2, NT = 2, NC = SW ? 1 : 2, PER = 128 / GS, MF = 4 / PER, TERMS = Terms<float>::N;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[2][TERMS][MB * 16 * 256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, g4 = lane >> 4;
+    const int m0 = blockIdx.y * (16 * MB), n0 = blockIdx.x * (64 * NC) + wave * (16 * NC), steps = (p.K + 127) / 128;
+    const int n_first = min(n0, p.N - 1);
+    const unsigned char* const base[2] = {p.w + size_t(n_first) * p.row_bytes, SW ? p.w2 + size_t(n_first) * p.row_bytes : nullptr};
+    const float* const sbase[2] = {(const float*)p.s + n_first, SW ? (const float*)p.s2 + n_first : nullptr};
+    unsigned row[NC], place[NC];
+#pragma unroll
+    for (int t = 0; t < NC; ++t) {
+        place[t] = min(n0 + 16 * t + n16, p.N - 1) - n_first;
+        row[t] = place[t] * p.row_bytes;
+    }
+    uint4 w[2][NT];
+    float s[2][NT][PER];
+    auto load = [&](int f, int i) {
+        const unsigned at = min(i * 64 + g4 * 16, p.row_bytes - 16);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            w[f][t] = *(const uint4*)(base[t / NC] + (row[t % NC] + at));
+#pragma unroll
+            for (int g = 0; g < PER; ++g) s[f][t][g] = (sbase[t / NC] + size_t(min(i * PER + g, p.groups - 1)) * p.N)[place[t % NC]];
+        }
+    };
+    const int piece = tid & 15, r0 = tid >> 4, put = r0 * 256 + ((piece ^ r0) << 4);
+    const float* from[MB];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) from[b] = (const float*)p.a + size_t(min(m0 + 16 * b + r0, p.M - 1)) * p.K;
+    f32x4 raw[MB][2];
+    auto load_rows = [&](int i) {
+        const int k = i * 128 + piece * 8, at = min(k, p.K - 8);
+#pragma unroll
+        for (int b = 0; b < MB; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) raw[b][h] = *(const f32x4*)(from[b] + at + 4 * h);
+    };
+    auto stage = [&](int i, int buf) {
+        const bool keep = i * 128 + piece * 8 < p.K;            // inputs past the last: zeros
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = keep ? raw[b][e / 4][e % 4] : 0.f;
+#pragma unroll
+            for (int q = 0; q < TERMS; ++q) {
+                bf16x8 x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { x[e] = bf16_t(y[e]); y[e] -= float(x[e]); }
+                *(bf16x8*)(lds[buf][q] + b * 4096 + put) = x;
+            }
+        }
+    };
+    f32x4 acc[MB][NT];
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](auto f_, int i) {
+        constexpr int f = decltype(f_)::value;
+        stage(i + 1, f ^ 1);
+        load_rows(min(i + 2, steps - 1));
+        load(f ^ 1, min(i + 1, steps - 1));
+        if constexpr (GS < 128)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) w[f][t] = transposed(w[f][t]);
+#pragma unroll
+        for (int g = 0; g < PER; ++g) {
+            f32x4 sum[MB][NT];
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) sum[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = g * MF; j < (g + 1) * MF; ++j) {
+                const int c = GS == 128 ? 4 * g4 + j : 4 * j + g4;
+                bf16x8 o[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) o[t] = operand<float>(word(w[f][t], j));
+#pragma unroll
+                for (int q = TERMS - 1; q >= 0; --q)
+#pragma unroll
+                    for (int b = 0; b < MB; ++b) {
+                        const bf16x8 x = *(const bf16x8*)(lds[f][q] + b * 4096 + n16 * 256 + ((c ^ n16) << 4));
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) sum[b][t] = mfma16(x, o[t], sum[b][t]);
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float sc = s[f][t][g] * 0.0625f;
+#pragma unroll
+                for (int b = 0; b < MB; ++b)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[b][t][v] = __builtin_fmaf(sum[b][t][v], sc, acc[b][t][v]);
+            }
+        }
+        __syncthreads();
+    };
+    load(0, 0);
+    load_rows(0);
+    stage(0, 0);
+    load_rows(min(1, steps - 1));
+    __syncthreads();
+    for (int i = 0; i < steps; i += 2) {
+        step(std::integral_constant<int, 0>{}, i);
+        if (i + 1 < steps) step(std::integral_constant<int, 1>{}, i + 1);
+    }
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int t = 0; t < NC; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int m = m0 + 16 * b + 4 * g4 + v, n = n0 + 16 * t + n16;
+                if (m >= p.M || n >= p.N) continue;
+                float* const d = (float*)p.out + size_t(m) * p.N + n;
+                if constexpr (SW) *d = silu_product<float>(acc[b][t][v], acc[b][t + NC][v]);
+                else if (p.epi == EPI_RESIDUAL_F32) *d += acc[b][t][v];
+                else *d = acc[b][t][v];
+            }
+}
+
 // Workgroups are dealt out to the eight XCDs in turn.  A column (the row tiles of the same outputs and inputs) stays on one, so that they share its
 // L2; neighbouring columns go to different ones.
 struct Place { int column, mt; };
@@ -831,6 +959,13 @@ hipError_t choose(const Product& p, float* ws, size_t ws_bytes, hipStream_t st) 
         if (p.M > 64 && p.M * outputs >= 800000 && need && need <= ws_bytes) return wide<SW>(p, GS, ws, ws_bytes, st);
         return tiles<SW, GS>(p, ws, ws_bytes, st);
     }
+    // Four rows at a time cost their share of the outputs and the inputs, tiles the inputs alone until the launch is full: rows / tiles, us: 732 rows, 3553 outputs,
+    // 1320 inputs 188 / 34; 64, 4096, 4096 53 / 46; 256, gate and up of 688, 256 14.1 / 6.0; 128, 1024, 1024 8.9 / 12.6; 40, 2048, 2048 10.5 / 22.
+    if constexpr (sizeof(T) == 4)
+        if (p.M > 16 && int64_t((p.M + 3) / 4) * p.N * (SW ? 2 : 1) >= 50000) {
+            hipLaunchKernelGGL((w4_f32_kernel<SW, GS>), dim3(unsigned((p.N + (SW ? 63 : 127)) / (SW ? 64 : 128)), unsigned((p.M + 31) / 32)), dim3(256), 0, st, p);
+            return hipGetLastError();
+        }
     return rows<T, SW, GS>(p, st);
 }
 

@@ -321,6 +321,34 @@ def test_many_rows_of_long_inputs(form):
     assert (off <= p.bound(a, "bf16")).all()
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(17, 10007, 136), (97, 1999, 264), (100, 2000, 520), (101, 2001, 8), (733, 300, 128), (257, 801, 1016), (32, 12345, 48), (64, 4096, 1032), (1024, 688, 256)])
+def test_many_rows_in_float32(group, M, N, K):
+    """Both sides of where tiles of 32 rows begin."""
+    check_plain("f32", M, N, K, group)
+
+
+@pytest.mark.parametrize("M,N,K,group", [(100, 1003, 264, 32), (257, 688, 256, 64), (130, 2049, 136, 128), (65, 1600, 1032, 32)])
+def test_many_rows_in_float32_residual_and_swiglu(M, N, K, group):
+    test_residual_and_swiglu("f32", M, N, K, group)
+
+
+@pytest.mark.parametrize("M,N", [(70, 3001), (300, 700)])
+def test_many_rows_in_float32_values_that_are_not_finite(M, N):
+    import torch
+    eng = engine("f32")
+    p = Projection(eng, N, 296, 64)
+    t, _ = activations(eng, M, 296)
+    clean = eng.op_gemm_w4(t, p.w4).clone()
+    t[1, 5], t[M - 1, 295] = float("nan"), float("inf")
+    p.w4.scales[33, 2], p.w4.scales[N - 1, 0] = float("nan"), float("inf")
+    got = eng.op_gemm_w4(t, p.w4)
+    rows, outputs = torch.ones(M, dtype=torch.bool, device="cuda"), torch.ones(N, dtype=torch.bool, device="cuda")
+    rows[[1, M - 1]], outputs[[33, N - 1]] = False, False
+    assert not torch.isfinite(got[~rows]).any() and not torch.isfinite(got[:, ~outputs]).any()
+    assert torch.equal(got[rows][:, outputs], clean[rows][:, outputs])
+
+
 @pytest.mark.parametrize("N,K", [(1, 136), (5, 24)])
 def test_a_description_keeps_its_scales(N, K):
     """One output, or one group: a layout in which the transposed scales are the scales themselves."""
