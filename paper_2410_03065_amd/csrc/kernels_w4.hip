@@ -928,9 +928,9 @@ hipError_t wide(Product p, int group, float* ws, size_t ws_bytes, hipStream_t st
     const std::integral_constant<int, 8> eight{};
     const int units = (p.N + 63) / 64, m_tiles = (p.M + 127) / 128;      // 64 outputs
     // 128 rows or 64: a workgroup's codes are converted once for its rows, but 64 make twice the workgroups, and up to 512 rows less padding.
-    // 128 against 64 rows, us: 1024 rows, 10240 outputs of 8192 inputs 162 / 243; 512, 4096 of 4096 40.1 / 35.0; 320, 14336 of 4096 76 / 64;
-    // 512, 14336 of 4096 76 / 87; 128, 28672 of 4096 49 / 53.
-    if (int64_t(p.M) * units < 65536 || (p.M < 512 && m_tiles * 2 != (p.M + 63) / 64)) return go(four, std::integral_constant<int, SW ? 2 : 1>{}, units, 0);
+    // 128 against 64 rows, us: 1024 rows, 10240 outputs of 8192 inputs 162 / 243; 857, 4096 of 11008 111 / 142; 640, 5120 of 5120 57.5 / 65.3; 768,
+    // 4096 of 4096 47.5 / 45.2; 512, 4096 of 14336 102 / 93; 320, 14336 of 4096 76 / 64; 128, 28672 of 4096 49 / 53.
+    if (int64_t(m_tiles) * units < 400 || (p.M < 512 && m_tiles * 2 != (p.M + 63) / 64)) return go(four, std::integral_constant<int, SW ? 2 : 1>{}, units, 0);
     // two workgroups a compute unit, in as few rounds as their widths allow
     const int slots = std::max(1, 512 / m_tiles), most = SW ? 2 : 4, rounds = (units + slots * most - 1) / (slots * most);
     const int tiles = std::min(units, rounds * slots), width = units / tiles, more = units - tiles * width;
