@@ -79,6 +79,19 @@ template <typename T> __device__ __forceinline__ bf16x8 operand(unsigned w) {
 }
 __device__ __forceinline__ bf16x8 minus24() { return __builtin_bit_cast(bf16x8, uint4{0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u}); }
 
+// The residual stream's elements of a wave's tiles, added to its sums: all read before any is written, which the compiler cannot know to be allowed and
+// would do one after the other (81 rows of 8716 outputs, 184 inputs: 15.4 us, so 8.0; 857 of 4096, 4096 inputs: 56, 46).  (m, n): of the lane's first element; past the last: the last, not stored.
+template <int MB, int NC, int NT>
+__device__ __forceinline__ void add_residual(const Product& p, int m, int n, f32x4 (&acc)[MB][NT]) {
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int t = 0; t < NC; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                acc[b][t][v] += ((const float*)p.out)[size_t(min(m + 16 * b + v, p.M - 1)) * p.N + min(n + 16 * t, p.N - 1)];
+}
+
 // Few rows.  A wave takes 16 NT outputs and an NW-th of the inputs in steps of 128, PF steps of codes ahead; a lane's 16 bytes of a row's codes
 // are 32 inputs of it.  Groups of 128: the four lanes of a row multiply their first eight, second eight .. at once.  Shorter groups: the
 // lanes exchange words first, so that a product's 32 inputs lie in one group.  The activations of R rows lie in LDS, in pieces of eight in the order
@@ -350,6 +363,7 @@ __device__ __forceinline__ void w4_tile(const Product& p, unsigned char* lds, in
             if (i + 3 < i1) step(std::integral_constant<int, 3>{}, i + 3);
         }
     }
+    if (!SW && splits == 1 && p.epi == EPI_RESIDUAL_F32) add_residual<MB, NC>(p, m0 + 4 * g4, n0 + n16, acc);
 #pragma unroll
     for (int b = 0; b < MB; ++b)
 #pragma unroll
@@ -364,7 +378,6 @@ __device__ __forceinline__ void w4_tile(const Product& p, unsigned char* lds, in
                     *d = acc[b][t][v];
                     if constexpr (SW) d[size_t(p.M) * p.N] = acc[b][t + NC][v];
                 } else if constexpr (SW) ((bf16_t*)p.out)[at] = silu_product<bf16_t>(acc[b][t][v], acc[b][t + NC][v]);
-                else if (p.epi == EPI_RESIDUAL_F32) ((float*)p.out)[at] += acc[b][t][v];
                 else ((float*)p.out)[at] = acc[b][t][v];
             }
 }
@@ -482,6 +495,7 @@ w4_f32_kernel(Product p) {
         step(std::integral_constant<int, 0>{}, i);
         if (i + 1 < steps) step(std::integral_constant<int, 1>{}, i + 1);
     }
+    if (!SW && p.epi == EPI_RESIDUAL_F32) add_residual<MB, NC>(p, m0 + 4 * g4, n0 + n16, acc);
 #pragma unroll
     for (int b = 0; b < MB; ++b)
 #pragma unroll
@@ -492,7 +506,6 @@ w4_f32_kernel(Product p) {
                 if (m >= p.M || n >= p.N) continue;
                 float* const d = (float*)p.out + size_t(m) * p.N + n;
                 if constexpr (SW) *d = silu_product<float>(acc[b][t][v], acc[b][t + NC][v]);
-                else if (p.epi == EPI_RESIDUAL_F32) *d += acc[b][t][v];
                 else *d = acc[b][t][v];
             }
 }
@@ -731,7 +744,14 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
         const int4 ru = *(const int4*)(q.row_unit + m0 + 16 * b + 4 * g4);
-        const auto value = [&](int t, int v) { return ldexpf(acc[b][t][v], (v == 0 ? ru.x : v == 1 ? ru.y : v == 2 ? ru.z : ru.w) + unit[t]); };
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[b][t][v] = ldexpf(acc[b][t][v], (v == 0 ? ru.x : v == 1 ? ru.y : v == 2 ? ru.z : ru.w) + unit[t]);
+    }
+    if (!SW && splits == 1 && p.epi == EPI_RESIDUAL_F32) add_residual<MB, NC>(p, m0 + 4 * g4, n0 + n16, acc);
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
 #pragma unroll
         for (int t = 0; t < NC; ++t)
 #pragma unroll
@@ -739,16 +759,13 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
                 const int m = m0 + 16 * b + 4 * g4 + v, n = n0 + 16 * t + n16;
                 if (m >= p.M || n >= p.N) continue;
                 const size_t at = size_t(m) * p.N + n;
-                const float y = value(t, v);
                 if (splits > 1) {
                     float* d = p.parts + size_t(split) * (SW ? 2 : 1) * p.M * p.N + at;
-                    *d = y;
-                    if constexpr (SW) d[size_t(p.M) * p.N] = value(t + NC, v);
-                } else if constexpr (SW) ((bf16_t*)p.out)[at] = silu_product<bf16_t>(y, value(t + NC, v));
-                else if (p.epi == EPI_RESIDUAL_F32) ((float*)p.out)[at] += y;
-                else ((float*)p.out)[at] = y;
+                    *d = acc[b][t][v];
+                    if constexpr (SW) d[size_t(p.M) * p.N] = acc[b][t + NC][v];
+                } else if constexpr (SW) ((bf16_t*)p.out)[at] = silu_product<bf16_t>(acc[b][t][v], acc[b][t + NC][v]);
+                else ((float*)p.out)[at] = acc[b][t][v];
             }
-    }
 }
 
 // Workgroups of two widths, so that a launch fills the compute units evenly: the first `more` of a row tile's `tiles` take 64 outputs more than the others.
@@ -951,8 +968,9 @@ hipError_t choose(const Product& p, float* ws, size_t ws_bytes, hipStream_t st) 
         const int64_t outputs = int64_t(p.N) * (SW ? 2 : 1);
         // Few rows: each four read the weights once more, which come from a cache then, but there is one launch and nothing between its workgroups.
         // rows / tiles, us: 4 rows, 4096 outputs of 4096 inputs 5.3 / 8.3, 16384 of 4096 10.8 / 13.0, 8192 of 8192 15.0 / 12.5, 28672 of 6144
-        // 32.7 / 24.9; 8 rows, 6144 of 4096 8.7 / 10.4, 12288 of 4096 15.5 / 13.3; 32 rows, 2048 of 2048 6.2 / 10.0; 16 rows, 4096 of 4096 9.1 / 8.6.
-        if (p.M == 1 || (p.M <= 4 && p.K <= 4096) || (p.M + 3) / 4 * outputs * p.K < int64_t(1) << 26) return rows<T, SW, GS>(p, st);
+        // 32.7 / 24.9; 8 rows, 6144 of 4096 8.7 / 10.4, 12288 of 4096 15.5 / 13.3; 32 rows, 2048 of 2048 6.2 / 10.0; 16 rows, 4096 of 4096 9.1 / 8.6;
+        // 100 rows, gate and up of 2000, 256 11.5 / 7.4.  Inputs below 1024 cost as much: eight waves share them.
+        if (p.M == 1 || (p.M <= 4 && p.K <= 4096) || (p.M + 3) / 4 * outputs * std::max(p.K, 1024) < int64_t(1) << 26) return rows<T, SW, GS>(p, st);
         // Many rows: the pass before the product costs some 8 us.  tiles / wide, us: 128 rows, 12288 outputs of 4096 inputs 36.4 / 28.9, 4096 of 14336
         // 33.4 / 34.9; 512 rows, 4096 of 4096 37.9 / 33.9, 1792 of 2048 23.6 / 18.3; up to 64 rows a tile's codes are converted once.
         const size_t need = wide_bytes(p, p.M);
