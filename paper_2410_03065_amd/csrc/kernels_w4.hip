@@ -695,46 +695,54 @@ __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, 
             o = next;
         }
     };
+    // The waits for the ring count what has been asked for since: the order of the loads is held, and check_lds_loads.py follows the listing's paths.
     if (i0 < i1) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int h = 0; h < RING - 1; ++h) bring(2 * i0 + h);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int f = 0; f < WS; ++f) load(f, min(i0 + f, i1 - 1));
+        __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NT * WS + (RING - 2) * DMA) : "memory");
         __builtin_amdgcn_s_barrier();
 #pragma unroll
         for (int b = 0; b < MB; ++b) x[b] = *(const f16x8*)(lds + 2 * i0 % RING * STAGE + b * 2048 + get[0]);
-        auto step = [&](auto f_, int i) {
-            constexpr int f = decltype(f_)::value;
+        // Behind the half step that must have come the next one was asked for and, while steps go on, a step's codes and scales (2 NT).  Of the last
+        // steps (more_ false) those are used by nobody, and the compiler drops them: there the next half step alone may be outstanding.
+        auto step = [&](auto f_, auto more_, int i) {
+            constexpr int f = decltype(f_)::value, CODES = decltype(more_)::value ? 2 * NT : 0;
             scales(f);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int h = 2 * i + half;
                 products(f, 2 * half, h % RING, 1);
                 __builtin_amdgcn_sched_barrier(0);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 3) * DMA + (RING - 2) * NT) : "memory");
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 3) * DMA + CODES) : "memory");
                 __builtin_amdgcn_s_barrier();
                 bring(h + RING - 1);
                 __builtin_amdgcn_sched_barrier(0);
                 products(f, 2 * half + 1, (h + 1) % RING, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            load(f, min(i + WS, i1 - 1));
+            if constexpr (CODES > 0) load(f, min(i + WS, i1 - 1));
             __builtin_amdgcn_sched_barrier(0);
         };
+        const std::true_type more{};
+        const std::false_type last{};
         int i = i0;
         for (; i + WS <= i1; i += WS) {
-            step(std::integral_constant<int, 0>{}, i);
-            step(std::integral_constant<int, 1>{}, i + 1);
+            step(std::integral_constant<int, 0>{}, more, i);
+            step(std::integral_constant<int, 1>{}, more, i + 1);
             if constexpr (WS == 4) {
-                step(std::integral_constant<int, 2>{}, i + 2);
-                step(std::integral_constant<int, 3>{}, i + 3);
+                step(std::integral_constant<int, 2>{}, more, i + 2);
+                step(std::integral_constant<int, 3>{}, more, i + 3);
             }
         }
-        if (i < i1) step(std::integral_constant<int, 0>{}, i);
+        if (i < i1) step(std::integral_constant<int, 0>{}, last, i);
         if constexpr (WS == 4) {
-            if (i + 1 < i1) step(std::integral_constant<int, 1>{}, i + 1);
-            if (i + 2 < i1) step(std::integral_constant<int, 2>{}, i + 2);
+            if (i + 1 < i1) step(std::integral_constant<int, 1>{}, last, i + 1);
+            if (i + 2 < i1) step(std::integral_constant<int, 2>{}, last, i + 2);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // what was asked for past the end
     }
