@@ -54,6 +54,12 @@ __device__ __forceinline__ unsigned word(uint4 x, int i) { return i == 0 ? x.x :
 
 template <typename T> struct Terms { static constexpr int N = 1; };
 template <> struct Terms<float> { static constexpr int N = 3; };       // 24 bits in three bfloat16
+// The nearest of the finite ones: what is left of an infinity, or of a number beyond the largest, is left to the next term, and an infinity
+// to the last, instead of inf - inf.
+__device__ __forceinline__ bf16_t finite_term(float y) {
+    constexpr float MOST = 0x1.fep127f;
+    return bf16_t(__builtin_amdgcn_fmed3f(y, -MOST, MOST));
+}
 
 struct Product {
     const void* a;
@@ -186,7 +192,7 @@ w4_rows_kernel(Product p, int held) {
                 for (int e = 0; e < 8; ++e) {
                     float y = k < p.K ? (e < 4 ? lo[e] : hi[e - 4]) : 0.f;
 #pragma unroll
-                    for (int q = 0; q < TERMS; ++q) { x[q][e] = bf16_t(y); y -= float(x[q][e]); }
+                    for (int q = 0; q < TERMS; ++q) { x[q][e] = q + 1 < TERMS ? finite_term(y) : bf16_t(y); y -= float(x[q][e]); }
                 }
 #pragma unroll
                 for (int q = 0; q < TERMS; ++q) *(bf16x8*)(to + q * 16 * R * 16) = x[q];
@@ -435,7 +441,7 @@ w4_f32_kernel(Product p) {
             for (int q = 0; q < TERMS; ++q) {
                 bf16x8 x;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { x[e] = bf16_t(y[e]); y[e] -= float(x[e]); }
+                for (int e = 0; e < 8; ++e) { x[e] = q + 1 < TERMS ? finite_term(y[e]) : bf16_t(y[e]); y[e] -= float(x[e]); }
                 *(bf16x8*)(lds[buf][q] + b * 4096 + put) = x;
             }
         }
