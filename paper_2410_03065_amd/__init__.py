@@ -364,8 +364,8 @@ class Engine:
     """Owns the device tensors (weights in ABI layout, KV pool, block tables), the pinned
     store and the two streams, and forwards to the C ABI.  The op_* calls wait for what torch's current
     stream was given before them (their operands come from there); the others do not: synchronise
-    after torch has written to the pool.  op_append_q8, op_attention_q8, their q4 forms, op_sample, pack_w4 and the op_gemm_w4 calls return
-    before their work is done: it runs in order with torch's current stream, without a wait where that is the compute stream.
+    after torch has written to the pool.  op_append_q8, op_attention_q8, their q4 forms, op_sample, w4 (a copy), pack_w4 and the op_gemm_w4 calls
+    return before their work is done: it runs on the compute stream, in order with torch's current stream, without a wait where that is the same.
     compute_stream: a torch stream of the default priority to use as the compute stream (None: one of the engine's own).
     An engine on torch's default stream runs such calls with the least delay, but they cannot be captured into a graph."""
 
@@ -942,14 +942,22 @@ class Engine:
     # -- products with 4-bit weights ------------------------------------------------------
     def w4(self, codes, scales, k, group=128) -> W4:
         """The description of a projection in 4 bits (cake_w4): codes uint8 [n][(k + 31) // 32 * 16], two a byte; scales [n][(k + group - 1) // group]
-        in the model's type, of which it keeps a copy laid out for the kernels.  It may be kept and used while the codes stay."""
+        in the model's type, of which it keeps a copy laid out for the kernels, made where their work runs: whichever stream is the current one when they are
+        called.  It may be kept and used while the codes stay."""
         if group not in (32, 64, 128) or k <= 0 or k % 8 or codes.dim() != 2 or codes.shape[0] == 0:
             raise CakeError(E_INVAL, "w4: codes %s for %d inputs, a scale for %d: rows of (k + 31) // 32 * 16 bytes, k by eights and groups of 32, 64 or 128 are needed" % (
                 tuple(codes.shape), k, group))
         n = codes.shape[0]
         at = self._operand(codes, "codes", self.torch.uint8, (n, (k + 31) // 32 * 16))
         self._operand(scales, "scales", self.tdtype, (n, (k + group - 1) // group))
-        return self._w4_of(codes, at, scales.t().clone(memory_format=self.torch.contiguous_format), n, k, group)
+        by_group = self.torch.empty(((k + group - 1) // group, n), dtype=self.tdtype, device=self.dev)
+
+        def copy(_):
+            with self.torch.cuda.stream(self.compute_stream):
+                by_group.copy_(scales.t())
+            return OK
+        self._in_order(copy, "w4")
+        return self._w4_of(codes, at, by_group, n, k, group)
 
     def _w4_of(self, codes, at, by_group, n, k, group):
         w = W4(at, by_group.data_ptr(), n, k, group)
