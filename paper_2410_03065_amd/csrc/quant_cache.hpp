@@ -1134,12 +1134,11 @@ merge_long_kernel(const float* __restrict__ part, T* __restrict__ out, Q8View v,
     const int tid = threadIdx.x, e0 = blockIdx.x % (HD / E) * E, row = int(i / n_q);
     if (row < v.row_begin[0] || row >= min(v.row_begin[v.n_seqs], v.n_rows)) return;
     const float* p = part + i * splits * (HD + 4);
-    float4 next[N];
+    f32x4 next[N];
     float2 ml;
     auto load = [&](int base) {                 // past the last: the last again, not used
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (base + C / N * k < splits) next[k] = *(const float4*)(p + size_t(min(base + tid / N + C / N * k, splits - 1)) * (HD + 4) + e0 + tid % N * 4);
+        for (int k = 0; k < N; ++k) next[k] = *(const f32x4*)(p + size_t(min(base + tid / N + C / N * k, splits - 1)) * (HD + 4) + e0 + tid % N * 4);
         ml = *(const float2*)(p + size_t(min(base + tid, splits - 1)) * (HD + 4) + HD);
     };
     load(0);
@@ -1163,7 +1162,7 @@ merge_long_kernel(const float* __restrict__ part, T* __restrict__ out, Q8View v,
     for (int base = 0; base < used; base += C) {
         if (base) __syncthreads();
 #pragma unroll
-        for (int k = 0; k < N; ++k) *(float4*)&x[tid / N + C / N * k][tid % N * 4] = next[k];
+        for (int k = 0; k < N; ++k) *(f32x4*)&x[tid / N + C / N * k][tid % N * 4] = next[k];
         weight[tid] = base + tid < used ? make_float2(__builtin_amdgcn_exp2f(ml.x - m), ml.y) : make_float2(0.f, 0.f);
         __syncthreads();
         if (base + C < used) load(base + C);
