@@ -869,6 +869,12 @@ class Engine:
                 name, dtype, "" if shape is None else " of %s" % (tuple(shape),), self.dev, t.dtype, tuple(t.shape), t.device))
         return t.data_ptr()
 
+    def _numbers(self, what, *numbers):
+        """A refusal of numbers that the C ABI's 32 bits do not hold: they would arrive as others."""
+        for x in numbers:
+            if not -1 << 31 <= x < 1 << 31:
+                raise CakeError(E_INVAL, "%s: %d does not fit 32 bits" % (what, x))
+
     def new_q8_pool(self, n_pages, page_tokens, scale_tokens=1):
         """A pool of 8-bit pages, zeros: uint8 [n_layers][n_pages][page bytes]."""
         return self.torch.zeros((self.shape.n_layers, n_pages, q8_page_bytes(self.shape, page_tokens, scale_tokens)),
@@ -885,6 +891,7 @@ class Engine:
             raise CakeError(E_INVAL, "%s: a pool of %d bytes for %d layers of pages of %d" % (what, pool.numel(), self.shape.n_layers, page))
         if block_table.dim() != 2:
             raise CakeError(E_INVAL, "%s: block_table must have a row per sequence" % what)
+        self._numbers(what, n_rows, page_tokens, scale_tokens, max_rows, max_len)
         n = block_table.shape[0]
         b = Q8Batch(self._operand(pool, "pool", torch.uint8), self._operand(block_table, "block_table", torch.int32),
                     self._operand(seq_len, "seq_len", torch.int32, (n,)), self._operand(row_begin, "row_begin", torch.int32, (n + 1,)),
@@ -906,6 +913,8 @@ class Engine:
                               page_tokens, scale_tokens, max_rows, max_len)
 
     def _append(self, fn, what, model, qkv, layer, batch, rope, q, want_values):
+        if layer >> 31:
+            self._numbers(what, layer)
         s, n = self.shape, self._batch(batch, model).n_rows
         if q is None:
             q = self.torch.empty((s.n_q, n, s.head_dim), dtype=self.tdtype, device=self.dev)
@@ -924,6 +933,8 @@ class Engine:
         return self._append(self.lib.cake_op_append_q4, "cake_op_append_q4", self._q4_model, qkv, layer, batch, rope, q, want_values)
 
     def _attention(self, fn, what, model, q, layer, batch, window, sinks, out):
+        if (layer | window | sinks) >> 31:
+            self._numbers(what, layer, window, sinks)
         s, n = self.shape, self._batch(batch, model).n_rows
         if out is None:
             out = self.torch.empty((n, s.n_q * s.head_dim), dtype=self.tdtype, device=self.dev)
@@ -948,6 +959,7 @@ class Engine:
             raise CakeError(E_INVAL, "w4: codes %s for %d inputs, a scale for %d: rows of (k + 31) // 32 * 16 bytes, k by eights and groups of 32, 64 or 128 are needed" % (
                 tuple(codes.shape), k, group))
         n = codes.shape[0]
+        self._numbers("w4", n, k)
         at = self._operand(codes, "codes", self.torch.uint8, (n, (k + 31) // 32 * 16))
         self._operand(scales, "scales", self.tdtype, (n, (k + group - 1) // group))
         by_group = self.torch.empty(((k + group - 1) // group, n), dtype=self.tdtype, device=self.dev)
@@ -970,6 +982,7 @@ class Engine:
         if w.dim() != 2 or w.shape[0] == 0 or w.shape[1] == 0 or w.shape[1] % 8 or group not in (32, 64, 128):
             raise CakeError(E_INVAL, "pack_w4: weights %s, a scale for %d: inputs by eights and groups of 32, 64 or 128 are needed" % (tuple(w.shape), group))
         n, k = w.shape
+        self._numbers("pack_w4", n, k)
         at = self._operand(w, "w", self.tdtype)
         codes = torch.empty((n, (k + 31) // 32 * 16), dtype=torch.uint8, device=self.dev)
         packed = self._w4_of(codes, codes.data_ptr(), torch.empty(((k + group - 1) // group, n), dtype=self.tdtype, device=self.dev), n, k, group)
@@ -986,6 +999,8 @@ class Engine:
     def _activations(self, a, w):
         if a.dim() != 2:
             raise CakeError(E_INVAL, "a: [rows][%d] is needed, got %s" % (w.k, tuple(a.shape)))
+        if a.shape[0] >> 31:
+            self._numbers("a: rows", a.shape[0])
         return self._operand(a, "a", self.tdtype, (a.shape[0], w.k)), a.shape[0]
 
     def op_gemm_w4(self, a, w, out=None):
