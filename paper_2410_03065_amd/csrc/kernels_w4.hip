@@ -882,16 +882,9 @@ hipError_t rows(const Product& p, hipStream_t st) {
     auto go = [&](auto r, auto nw) {
         constexpr int R = decltype(r)::value, PF = sizeof(T) == 2 ? 2 : 1, NW = decltype(nw)::value, STEP = Terms<T>::N * 256 * R;
         const int held = std::min((p.K + 127) / 128, (sizeof(T) == 2 ? 32 << 10 : 24 << 10) / STEP);
-        constexpr int MOST = 65535 * R;                    // a grid's second size
-        for (int m = 0; m < p.M; m += MOST) {
-            Product q = p;
-            q.M = std::min(p.M - m, MOST);
-            q.a = (const T*)p.a + size_t(m) * p.K;
-            q.out = (char*)p.out + size_t(m) * p.N * (SW ? sizeof(T) : sizeof(float));
-            hipLaunchKernelGGL((w4_rows_kernel<T, SW, R, NT, GS, NW, PF>), dim3(unsigned((p.N + 15) / 16), unsigned((q.M + R - 1) / R)), dim3(64 * NW), held * STEP, st, q, held);
-            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        }
-        return hipSuccess;
+        // a grid's second size, at most 65535: `choose` sends fewer than 2^16 fours of rows here, whatever their outputs and inputs
+        hipLaunchKernelGGL((w4_rows_kernel<T, SW, R, NT, GS, NW, PF>), dim3(unsigned((p.N + 15) / 16), unsigned((p.M + R - 1) / R)), dim3(64 * NW), held * STEP, st, p, held);
+        return hipGetLastError();
     };
     auto by_waves = [&](auto r) {
         const std::integral_constant<int, 8> eight{};

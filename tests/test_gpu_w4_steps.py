@@ -55,3 +55,9 @@ def test_the_same_bits_again_and_beside_other_rows(form, M, N, steps):
         assert torch.equal(run(), first)
     t[:M // 2] = -3.0
     assert torch.equal(run()[M // 2:], first[M // 2:])
+
+
+@pytest.mark.parametrize("kind,M", [("bf16", 262140), ("bf16", 262141), ("f32", 199996), ("f32", 199997)])
+def test_the_most_rows_four_at_a_time(kind, M):
+    """One output: the last number of rows that goes four at a time (65535 fours of bf16 models, as many as a grid takes), and the next."""
+    check_plain(kind, M, 1, 8, 32)
