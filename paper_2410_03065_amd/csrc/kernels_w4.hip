@@ -55,7 +55,7 @@ __device__ __forceinline__ unsigned word(uint4 x, int i) { return i == 0 ? x.x :
 template <typename T> struct Terms { static constexpr int N = 1; };
 template <> struct Terms<float> { static constexpr int N = 3; };       // 24 bits in three bfloat16
 // The nearest of the finite ones: what is left of an infinity, or of a number beyond the largest, is left to the next term, and an infinity
-// to the last, instead of inf - inf.
+// to the last, instead of inf - inf.  An instruction an element and term: 732 rows, 3553 outputs, 1320 inputs, groups of 32 36.3 us, without 34.4; few rows 2 % more.
 __device__ __forceinline__ bf16_t finite_term(float y) {
     constexpr float MOST = 0x1.fep127f;
     return bf16_t(__builtin_amdgcn_fmed3f(y, -MOST, MOST));
@@ -98,7 +98,8 @@ __device__ __forceinline__ void add_residual(const Product& p, int m, int n, f32
                 acc[b][t][v] += ((const float*)p.out)[size_t(min(m + 16 * b + v, p.M - 1)) * p.N + min(n + 16 * t, p.N - 1)];
 }
 
-// Few rows.  A wave takes 16 NT outputs and an NW-th of the inputs in steps of 128, PF steps of codes ahead; a lane's 16 bytes of a row's codes
+// Few rows.  A wave takes 16 NT outputs and an NW-th of the inputs in steps of 128 and asks for codes PF steps ahead (the compiler's waits, one for all ways that lead
+// to a step, leave the newest load or none of them on its way, so the waves of a compute unit cover the rest); a lane's 16 bytes of a row's codes
 // are 32 inputs of it.  Groups of 128: the four lanes of a row multiply their first eight, second eight .. at once.  Shorter groups: the
 // lanes exchange words first, so that a product's 32 inputs lie in one group.  The activations of R rows lie in LDS, in pieces of eight in the order
 // of the codes: loads come back in order, and one of a row's that waits behind the codes would take their depth away.  They are brought for
@@ -232,8 +233,9 @@ w4_rows_kernel(Product p, int held) {
 // tiles, rows of 256 bytes whose 16-byte pieces lie at piece ^ row, so that 16 rows' pieces of one number lie in different banks.  Who brings a
 // piece also adds up its activations, for -24 times the sum of a row's group: where a group's sum begins.
 // A unit is a group of a tile of 16 outputs.  While its products run, the next unit's codes are converted and the last one's sums scaled.
-// Bound by the time from a load to its use: a launch's workgroups live for a few steps, and the ranges are joined by a second launch (3 to 4 us).
-// Measured: 33 rows, 4096 outputs of 14336 inputs, groups of 64: 19.5 us, 1.6 TB/s.
+// Bound by the time from a load to its use: a launch's workgroups live for a few steps, a turn's first step also waits for the codes that the step before has just
+// asked for (all ways to the loop's beginning have one wait), and the ranges are joined by a second launch (3 to 4 us).
+// Measured: 33 rows, 4096 outputs of 14336 inputs, groups of 64: 19.2 us, 1.6 TB/s.
 template <bool SW, int MB, int NT, int GS, int WS, int XS>
 __device__ __forceinline__ void w4_tile(const Product& p, unsigned char* lds, int mt, int n_begin, int split, int splits) {
     constexpr int NC = SW ? NT / 2 : NT, PER = 128 / GS, MF = 4 / PER, UNITS = PER * NT, TILE = MB * 16 * 256, SUMS = PER * MB * 16 * 4;
@@ -390,7 +392,8 @@ __device__ __forceinline__ void w4_tile(const Product& p, unsigned char* lds, in
 
 // Many rows of float32 models.  As above, with three terms of each activation in LDS and two tiles of 16 rows; a code's conversion (twice a
 // bfloat16 one's instructions) serves 32 rows, a fragment of activations two tiles of outputs.  Bound by those conversions and by the time of a
-// step, some 1.2 us, while a launch has few workgroups.  Measured: 732 rows, 3553 outputs, 1320 inputs: 34 us, four rows at a time 188.
+// step, some 1.2 us, while a launch has few workgroups (the inputs are not divided).  Measured: 732 rows, 3553 outputs, 1320 inputs: 36 us (groups of 32; of 128: 34), four
+// rows at a time 206.
 template <bool SW, int GS>
 __global__ void __launch_bounds__(256, 2)
 w4_f32_kernel(Product p) {
@@ -624,8 +627,9 @@ __device__ __forceinline__ f16x8 weights8(unsigned w, f16x2 s) {
 // A workgroup takes 16 MB rows and 64 NC outputs (SwiGLU: of each matrix), a wave all of the rows and 16 NC outputs.  Activations come into LDS in
 // halves of a step, a ring of RING, by loads that pass no register; codes into registers, steps ahead.  Half-way through a half step all its
 // operands are read: there the waves meet, the next half must have come, and the last of the ring is asked for, into the place of the half before.
-// Loads come back in order, so the ring has to reach as far ahead as the codes.  Measured: 1024 rows, 10240 outputs of 8192 inputs: 148 us, 1.16
-// PFLOP/s, of the 1.20 that a library's large bfloat16 product reaches here; 11 us more for the pass before.
+// Loads come back in order, so the ring has to reach as far ahead as the codes; a turn of the loop begins with a wait for its first codes, which takes in loads of the
+// half step before.  Measured: 1024 rows, 10240 outputs of 8192 inputs: 147 us, 1.17 PFLOP/s, of the 1.20 that a library's large bfloat16 product reaches
+// here; 10 us more for the pass before (157 for both under the profiler, the call without it 154).
 #define CAKE_LDS_AS __attribute__((address_space(3)))
 template <bool SW, int MB, int NT>
 __device__ __forceinline__ void w4_wide_tile(const Wide& q, unsigned char* lds, int mt, int n_begin, int split, int splits) {
@@ -952,8 +956,8 @@ hipError_t wide(Product p, int group, float* ws, size_t ws_bytes, hipStream_t st
     const std::integral_constant<int, 8> eight{};
     const int units = (p.N + 63) / 64, m_tiles = (p.M + 127) / 128;      // 64 outputs
     // 128 rows or 64: a workgroup's codes are converted once for its rows, but 64 make twice the workgroups, and up to 512 rows less padding.
-    // 128 against 64 rows, us: 1024 rows, 10240 outputs of 8192 inputs 162 / 243; 857, 4096 of 11008 111 / 142; 640, 5120 of 5120 57.5 / 65.3; 768,
-    // 4096 of 4096 47.5 / 45.2; 512, 4096 of 14336 102 / 93; 320, 14336 of 4096 76 / 64; 128, 28672 of 4096 49 / 53.
+    // 128 against 64 rows, us: 1024 rows, 10240 outputs of 8192 inputs 156 / 237; 857, 4096 of 11008 106 / 137; 640, 5120 of 5120 53.8 / 62.6; 768,
+    // 4096 of 4096 45.6 / 44.6; 512, 4096 of 14336 86.8 / 89.9; 320, 14336 of 4096 71.6 / 63.6; 128, 28672 of 4096 45.3 / 50.6.
     if (int64_t(m_tiles) * units < 400 || (p.M < 512 && m_tiles * 2 != (p.M + 63) / 64)) return go(four, std::integral_constant<int, SW ? 2 : 1>{}, units, 0);
     // two workgroups a compute unit, in as few rounds as their widths allow
     const int slots = std::max(1, 512 / m_tiles), most = SW ? 2 : 4, rounds = (units + slots * most - 1) / (slots * most);
@@ -974,18 +978,19 @@ hipError_t choose(const Product& p, float* ws, size_t ws_bytes, hipStream_t st) 
     if constexpr (sizeof(T) == 2) {
         const int64_t outputs = int64_t(p.N) * (SW ? 2 : 1);
         // Few rows: each four read the weights once more, which come from a cache then, but there is one launch and nothing between its workgroups.
-        // rows / tiles, us: 4 rows, 4096 outputs of 4096 inputs 5.3 / 8.3, 16384 of 4096 10.8 / 13.0, 8192 of 8192 15.0 / 12.5, 28672 of 6144
-        // 32.7 / 24.9; 8 rows, 6144 of 4096 8.7 / 10.4, 12288 of 4096 15.5 / 13.3; 32 rows, 2048 of 2048 6.2 / 10.0; 16 rows, 4096 of 4096 9.1 / 8.6;
-        // 100 rows, gate and up of 2000, 256 11.5 / 7.4.  Inputs below 1024 cost as much: eight waves share them.
+        // rows / tiles, us: 4 rows, 4096 outputs of 4096 inputs 5.3 / 8.7, 16384 of 4096 10.8 / 13.0, 8192 of 8192 14.8 / 12.5, 28672 of 6144
+        // 32.2 / 25.0; 8 rows, 6144 of 4096 8.6 / 10.2, 12288 of 4096 15.6 / 13.3; 32 rows, 2048 of 2048 6.2 / 10.0; 16 rows, 4096 of 4096 9.2 / 8.7;
+        // 100 rows, gate and up of 2000, 256 11.5 / 7.3.  Inputs below 1024 cost as much: eight waves share them.
         if (p.M == 1 || (p.M <= 4 && p.K <= 4096) || (p.M + 3) / 4 * outputs * std::max(p.K, 1024) < int64_t(1) << 26) return rows<T, SW, GS>(p, st);
-        // Many rows: the pass before the product costs some 8 us.  tiles / wide, us: 128 rows, 12288 outputs of 4096 inputs 36.4 / 28.9, 4096 of 14336
-        // 33.4 / 34.9; 512 rows, 4096 of 4096 37.9 / 33.9, 1792 of 2048 23.6 / 18.3; up to 64 rows a tile's codes are converted once.
+        // Many rows: the pass before the product costs some 8 us.  tiles / wide, us: 128 rows, 12288 outputs of 4096 inputs 36.6 / 28.4, 4096 of 14336
+        // 33.5 / 34.4; 512 rows, 4096 of 4096 38.8 / 33.3, 1792 of 2048 22.5 / 17.7; 2048 rows, 4096 of 14336 354 / 245; up to 64 rows a tile's codes are
+        // converted once.  Without room for the pass's activations in the workspace it is the tiles: 4096 rows, 4096 of 14336 705.
         const size_t need = wide_bytes(p, p.M);
         if (p.M > 64 && p.M * outputs >= 800000 && need && need <= ws_bytes) return wide<SW>(p, GS, ws, ws_bytes, st);
         return tiles<SW, GS>(p, ws, ws_bytes, st);
     }
     // Four rows at a time cost their share of the outputs and the inputs, tiles the inputs alone until the launch is full: rows / tiles, us: 732 rows, 3553 outputs,
-    // 1320 inputs 188 / 34; 64, 4096, 4096 53 / 46; 256, gate and up of 688, 256 14.1 / 6.0; 128, 1024, 1024 8.9 / 12.6; 40, 2048, 2048 10.5 / 22.
+    // 1320 inputs 206 / 37; 64, 4096, 4096 54 / 48; 256, gate and up of 688, 256 13.8 / 5.7; 128, 1024, 1024 8.4 / 13.2; 40, 2048, 2048 10.5 / 23.7.
     if constexpr (sizeof(T) == 4)
         if (p.M > 16 && int64_t((p.M + 3) / 4) * p.N * (SW ? 2 : 1) >= 50000) {
             hipLaunchKernelGGL((w4_f32_kernel<SW, GS>), dim3(unsigned((p.N + (SW ? 63 : 127)) / (SW ? 64 : 128)), unsigned((p.M + 31) / 32)), dim3(256), 0, st, p);

@@ -395,9 +395,9 @@ template <int W> __device__ __forceinline__ KeySteps<W> key_steps(int pos_lo, in
 // sum, and 24 times the weights' sums, one more product a step, are taken from the outputs at the end: the same numbers in float32 but for
 // roundings of 24 times a wave's sum of weights, below 2^-24 24 of it each, where a bfloat16 output's own is 2^-8 of it.
 // Measured: 64 sequences of 500 to 8191 keys, 8 KV heads of 128: 126 us, 4.7 TB/s; 24 of 4100 visible keys, 32 KV heads: 147 us, 5.5 TB/s.
-// 4 bits: 81 us (as 16 c 98), 3.7 TB/s; 32 of 30001 keys 219 us (259), 4.8 TB/s; one of 100001 28.5 us (with the merge), 3.8 TB/s.
-// With 4 bits the vector instructions weigh as much as the bytes: 33 sequences of 37 to 9001, 20 rows, a window of 4096, heads of 64, 33 us of
-// which they take 20.
+// 4 bits: 81 us (as 16 c 98), 3.7 TB/s; 32 of 30001 keys 219 us (259), 4.8 TB/s; one of 100001 29.7 us (with the merge), 3.7 TB/s (26.4 where the pages come from a
+// cache).  With 4 bits the vector instructions weigh as much as the bytes, half of the cycles: 33 sequences of 37 to 9001, 20 rows, a window of 4096, heads of
+// 64, 32 us, of which they take 16.
 template <typename T> struct Terms { static constexpr int Q = 1, W = 2; };
 template <> struct Terms<float> { static constexpr int Q = 3, W = 3; };
 
@@ -702,7 +702,7 @@ attention_kernel(const T* __restrict__ q, T* __restrict__ out, float* __restrict
 // first of them before the barrier.
 // Bound by the vector instructions beside the products: a score takes 5 and an exponential (four times the issue of one), a
 // code 1.5 over the workgroup's rows.  1024 rows of 32 heads after 15360 keys, 8 KV heads of 128: 330 to 390 us with the clock, 0.7 to
-// 0.8 PFLOP/s; with products, weights and the rest each left alone, 131, 81 and 195.  4 bits: 307 us (keys as 16 c: 314).
+// 0.8 PFLOP/s; with products, weights and the rest each left alone, 131, 81 and 195.  4 bits: 325 us (keys as 16 c 2 % more).
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
 __device__ __forceinline__ f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -1121,7 +1121,7 @@ merge_kernel(const float* __restrict__ part, T* __restrict__ out, Q8View v, int 
 }
 
 // The same sums in the same order, for few rows of many ranges: a workgroup takes 32 elements of a row, all of whose ranges are asked for at once, 256 at a time.
-// 32 rows of 241 ranges: 10 us, and 54 from memory in order, where a range waits for the one four before.  Whole rows to a workgroup: 30.
+// Bound by its two waits, for the weights and for the elements.  32 rows of 96 ranges: 4.7 us; from memory in order, where a range waits for the one four before, some 22.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256)
 merge_long_kernel(const float* __restrict__ part, T* __restrict__ out, Q8View v, int n_q, int splits) {
@@ -1241,7 +1241,8 @@ hipError_t merge(const Q8View& v, int n_q, const KeyRanges& k, const AttnWs& ws,
     if (e != hipSuccess || k.splits == 1) return e;
     const size_t rows = size_t(v.n_rows) * n_q;
     // With many ranges of few rows the way through LDS (us, attention and this, 4 bits, 8 KV heads of 128, against a lane's eight elements in order from
-    // memory): 32 rows, 241 ranges 43, 87; 32, 71 12.9, 24.9; 32, 32 9.1, 13.0; 256, 235 64, 90; 128, 64 44, 52; 256, 32 82, 78; 512, 32 104, 93.
+    // memory): 32 rows, 96 ranges 26.2, 43.9; 32, 94 15.5, 32.3; 32, 71 10.7, 24.4; 256, 20 57.2, 58.4; 256, 16 21.8, 22.6; 512, 8 40.9, 38.0; 640, 16
+    // 25.4, 22.1.  128 rows of 29 ranges, 17.2, 21.4, still go the other way: the border dates from when a range here waited for the one before.
     if (k.splits > 8 && rows * v.head_dim <= size_t(512) * k.splits) {
         if (v.head_dim == 128) hipLaunchKernelGGL((merge_long_kernel<T, 128>), dim3(unsigned(rows * 4)), dim3(256), 0, st, ws.part, out, v, n_q, k.splits);
         else hipLaunchKernelGGL((merge_long_kernel<T, 64>), dim3(unsigned(rows * 2)), dim3(256), 0, st, ws.part, out, v, n_q, k.splits);
@@ -1257,9 +1258,9 @@ template <int BITS, typename T, int HD, int NB, int NS>
 hipError_t attention(const T* q, T* out, const Q8View& v, int n_q, int max_rows, int max_len, int window, int sinks, float scale, const AttnWs& ws, hipStream_t st) {
     if (BITS == 4 && Terms<T>::Q == 1) scale /= UNIT<BITS>;         // codes as 24 + c, not 16 c
     // Of 4 bits, half the bytes a step, a workgroup's beginning and its part of the result weigh more: one round of workgroups, where the sequences'
-    // lengths do not differ.  512 / 768 / 1024 / 2048 (us, heads of 128): 1 of 100001 35.4, 29.6, 32.5, 38.6; 2 of 60001 36.3, 32.6, 37.7, 39.0; 4 of
-    // 500 to 30001 34.9, 31.4, 29.3, 33.1; 16 of 500 to 9001 32.5, 32.4, 28.8, 31.3; tiles of 32 rows: 1 of 60001 41.2, 41.8, 46.7, 63.8; 4 of 500
-    // to 30001 44, 56, 55, 61; heads of 64: 1 of 100001 28.4, 23.8, 24.0, 29.9.
+    // lengths do not differ.  512 / 768 / 1024 / 2048 (us, heads of 128): 1 of 100001 31.1, 26.2, 28.9, 33.6; 2 of 60001 31.1, 28.2, 32.7, 33.8; 4 of
+    // 500 to 30001 33.1, 30.7, 25.8, 29.7; 16 of 500 to 9001 30.4, 30.4, 27.3, 30.0; tiles of 32 rows: 1 of 60001 28.7, 31.9, 34.4, 44.6; 4 of 500
+    // to 30001 39, 50, 50, 55; heads of 64: 1 of 100001 24.5, 20.7, 20.8, 25.7.
     const int want = BITS == 8 ? 2048 : NB == 2 ? 512 : HD == 128 && v.n_seqs <= 2 ? 768 : 1024;
     const KeyRanges k = key_ranges(v, n_q, 16 * NB, 32, max_rows, max_len, window, sinks, 4, 48, want, ws);
     // Undivided on eight waves, without a merge, where sequences are not too long for it: one such workgroup fills a compute unit, so the
@@ -1330,6 +1331,8 @@ hipError_t launch_attention(int dtype, const void* q, void* out, const Q8View& v
         // 16 sequences of 8191 keys: 36 rows 82, 144, -; 96 rows 159, 145, 251; 192 rows 253, 264, 251; 256 rows 326, 266, 251;
         // 16 ragged ones up to 4099: 36 rows 40, 78, -; 128 rows 73, 81, 116; 132 rows 73, 133, 128; 256 rows 101, 140, 128;
         // 1 of 16000: 36 rows 46, 42, -; 128 rows 53, 44, -; 256 rows 79, 52, 48; 4 of 4096, 512 rows: 97, 82, 75.
+        // All with 8 bits; the two were not measured against each other with 4, whose tiles of 16 rows convert longer: 16 of 8191, 96 rows (tiles of 16) 142, 128 rows (one
+        // tile) 110, so 96 rows are some 30 dearer than that tile would be.
         if constexpr (HD == 128) {
             const int64_t few = 2 * ((rows + 15) / 16), four = 13 * ((rows + 127) / 128), eight = 24 * ((rows + 255) / 256);
             if (four < few && four < eight) return attention_rows<BITS, HD, 4, NS>(qb, ob, v, n_q, max_rows, max_len, window, sinks, scale, ws, st);
