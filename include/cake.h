@@ -669,9 +669,10 @@ int32_t cake_op_pack_w4(cake_ctx* ctx, const void* w, void* codes, void* scales,
  * (bf16 models; more than 64, and 800 000 sums or more) the scale is multiplied into the codes first, exactly for scales down to 2^-27 of their output's largest
  * and activations down to 2^-31 of their row's largest, and smaller ones lose at most 2^-35 and 2^-39 of the largest.  That takes workspace for the activations (2 M K
  * bytes, each rounded up to 128s, and 4 bytes a row and output), of which a context has 64 MB or, if it is made for short chunks, less; a call without room goes the first
- * way and takes half as long again: two calls of half the rows are faster.  The order of the sums depends on M and on the context's size.  bf16 models: a result whose row holds an infinity, or activations beyond 2^115, may be a NaN
- * where a sum of plain products would be infinite.  float32 models: an infinity counts as in plain products; 16 times the codes are added up, so a
- * group with activations beyond 2^113 may give an infinity, or a NaN, whatever its scale; what an activation has below 2^-133 is lost.
+ * way and takes half as long again: two calls of half the rows are faster.  The order of the sums depends on M and on the context's size.
+ * bf16 models: a result whose row holds an infinity, or activations beyond 2^115, may be a NaN where a sum of plain products would be infinite.
+ * float32 models: an infinity counts as in plain products; 16 times the codes are added up, so a group with activations beyond 2^113 may give an
+ * infinity, or a NaN, whatever its scale; what an activation has below 2^-133 is lost.
  * M, N and K <= 2^20, M N <= 2^35.  The result must not overlap what is read.
  * Errors: CAKE_E_INVAL, CAKE_E_HIP. */
 int32_t cake_op_gemm_w4(cake_ctx* ctx, const void* a, const cake_w4* w, float* out, int32_t M);

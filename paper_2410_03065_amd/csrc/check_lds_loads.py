@@ -11,7 +11,7 @@ compiler's assembly listing of the kernel source (produced by the build; nothing
 A barrier is a tile's first until loads into LDS have been outstanding at one; where none is any more, the next is a first again (a kernel
 holds tiles of two widths).
 
-Vector loads return in the order they were issued; stores are not counted on to (a wait for n operations may leave the last n loads).
+Vector loads return in the order they were issued; stores are not counted on (a wait for n operations may leave the last n loads).
 A half step is MB / 2 loads a wave, MB being the kernel's second template argument.
 
     python check_lds_loads.py listing.s w4_wide_kernel
